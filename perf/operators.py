@@ -380,7 +380,9 @@ def work(case):
         if kind == "norm":
             return {"bytes": 2 * n * ((4 if case["block"] else 2) + (case["gate"] == "token")) + w,
                     "flops": n * (5 + (3 if case["block"] else 0) + 5 * case["post"])}
-        return {"bytes": 2 * n * (6 + 2 * (case["gate"] == "token")) + 3 * w, "flops": n * (16 + 14 * case["post"])}
+        # the block's output counts where its norm or gate is to be differentiated
+        rows = 5 + (case["post"] or case["gate"] != "none") + 2 * (case["gate"] == "token")
+        return {"bytes": 2 * n * rows + 3 * w, "flops": n * (16 + 14 * case["post"])}
     if kind == "embed":
         n = case["rows"] * case["hidden"]
         return {"bytes": 2 * n + 2 * _distinct(case["rows"], case["vocab"]) * case["hidden"] + 4 * case["rows"], "flops": n}
