@@ -23,7 +23,7 @@
  *   - the caller owns every buffer; the library never allocates, frees or
  *     synchronizes; each call enqueues kernels on `stream` (a hipStream_t,
  *     NULL for the default stream) and returns;
- *   - outputs must not alias inputs;
+ *   - outputs must not alias inputs, but where a call says that they may;
  *   - integer data that lives on the device (cu_seqlens, seqlens,
  *     block_table, targets) is trusted: it is not read by the host.  Setting
  *     the environment variable UATTN_VALIDATE=1 makes the host copy it back
@@ -371,6 +371,215 @@ uattn_status uattn_prefill_backward(const void* q, const void* k, const void* v,
                                     int32_t total_tokens, int32_t max_seqlen, int32_t num_q_heads,
                                     int32_t num_kv_heads, int32_t head_dim, float softmax_scale, void* dq, void* dk,
                                     void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The seam between two blocks in one pass: the norm behind a block, its gate
+ * and scale, the residual sum, and the norm before the next block (the hidden
+ * and fused residual RMSNorm of Section 6 Q3's operator table).  For every
+ * token's row, with r(a) = 1 / sqrt(mean_i a_i^2 + eps):
+ *
+ *   u = x * r(x) * post_weight         (u = x without post_weight)
+ *   s = residual + scale * gate * u    (gate 1 without gate; s = residual without x)
+ *   residual_out = bf16(s),  y = bf16(s * r(s) * pre_weight)
+ *
+ * in fp32, each output rounded once (the second norm reads s, not its rounding);
+ * the mean of a row's squares has to fit fp32.
+ *
+ *   x             [num_tokens, hidden_dim] bf16, the block's output, or NULL:
+ *                 then y is the norm of residual, and post_weight, gate and
+ *                 residual_out are NULL too
+ *   post_weight   [hidden_dim] bf16, or NULL
+ *   gate          bf16, or NULL: one row for all tokens (gate_stride 0) or
+ *                 [num_tokens, hidden_dim] (gate_stride hidden_dim)
+ *   scale         finite; multiplies the block's branch
+ *   residual      [num_tokens, hidden_dim] bf16
+ *   pre_weight    [hidden_dim] bf16, or NULL together with y
+ *   residual_out  [num_tokens, hidden_dim] bf16 (written; may be residual itself)
+ *   y             [num_tokens, hidden_dim] bf16 (written; may be x, or residual
+ *                 where x is NULL)
+ *
+ * hidden_dim a multiple of 8, at most 16384 (UATTN_EUNSUPPORTED otherwise);
+ * eps >= 0 and finite; tensors contiguous and 16-byte aligned.  A row's sums are
+ * taken in an order that depends only on hidden_dim, so a row's bits are the
+ * same in any batch.  A row of zeros with eps 0 gives NaN.
+ */
+uattn_status uattn_residual_norm(const void* x, const void* post_weight, const void* gate, int64_t gate_stride,
+                                 float scale, const void* residual, const void* pre_weight, float eps,
+                                 int32_t num_tokens, int32_t hidden_dim, void* residual_out, void* y, void* stream);
+
+/*
+ * Bytes of device workspace uattn_residual_norm_backward needs: the partial
+ * column sums of up to 256 groups of rows.  Pure host arithmetic; 0 for invalid sizes.
+ */
+size_t uattn_residual_norm_backward_workspace_bytes(int32_t num_tokens, int32_t hidden_dim);
+
+/*
+ * The gradients of uattn_residual_norm, at the stored rows h = residual_out
+ * and x.  With n = h r(h), m = x r(x), and sums over the tokens:
+ *
+ *   a = dy pre_weight;       ds = dresidual_out + r(h) (a - n mean(a n));   dpre_weight = sum dy n
+ *   dresidual = ds;          dgate = scale ds u (a row of sums for a shared gate)
+ *   b = scale ds gate;       dpost_weight = sum b m
+ *   c = b post_weight;       dx = r(x) (c - m mean(c m))   (dx = b without post_weight)
+ *
+ *   dy             [num_tokens, hidden_dim] bf16, or NULL where the forward had no y
+ *                  (pre_weight, dpre_weight and dy are NULL together)
+ *   dresidual_out  [num_tokens, hidden_dim] bf16, or NULL (zeros); not NULL with dy
+ *   residual_out   [num_tokens, hidden_dim] bf16, the forward's (the residual
+ *                  itself where it had no x); read only with dy
+ *   x              as passed to the forward; may be NULL where neither
+ *                  post_weight nor gate is given (their gradients alone read it)
+ *   post_weight, gate, gate_stride, scale, eps   as passed to the forward
+ *   dresidual      [num_tokens, hidden_dim] bf16 (written; may be dresidual_out itself)
+ *   dx             [num_tokens, hidden_dim] bf16 (written; may be dy), or NULL where
+ *                  the forward had no x
+ *   dpre_weight, dpost_weight   [hidden_dim] fp32 (written; zeros for no tokens)
+ *   dgate          fp32 [hidden_dim] for a shared gate, bf16 [num_tokens, hidden_dim]
+ *                  for a gate of every token (written)
+ *   workspace      at least uattn_residual_norm_backward_workspace_bytes bytes,
+ *                  16-byte aligned, no initial contents needed; calls sharing a
+ *                  workspace must be ordered on one stream
+ *
+ * No atomics: repeated calls give the same bits, and a row of dresidual, dx and
+ * a token's dgate the same bits in any batch.
+ */
+uattn_status uattn_residual_norm_backward(const void* dy, const void* dresidual_out, const void* residual_out,
+                                          const void* pre_weight, const void* x, const void* post_weight,
+                                          const void* gate, int64_t gate_stride, float scale, float eps,
+                                          int32_t num_tokens, int32_t hidden_dim, void* dresidual, void* dx,
+                                          float* dpre_weight, float* dpost_weight, void* dgate, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/*
+ * Embedding lookup:  out[t] = bf16(scale * table[ids[t]]).
+ *
+ *   ids     [num_tokens] int32; a negative id is padding and gives a row of
+ *           zeros, one of vocab or more a row of NaN (refused under UATTN_VALIDATE)
+ *   table   [vocab, table_stride] bf16, first hidden_dim used
+ *   scale   finite
+ *   out     [num_tokens, out_stride] bf16, first hidden_dim written
+ *   hidden_dim a multiple of 8; strides >= hidden_dim and multiples of 8
+ *   elements; pointers 16-byte aligned.
+ */
+uattn_status uattn_embedding(const int32_t* ids, const void* table, int64_t table_stride, float scale,
+                             int32_t num_tokens, int32_t vocab, int32_t hidden_dim, void* out, int64_t out_stride,
+                             void* stream);
+
+/*
+ * Bytes of device workspace uattn_embedding_backward needs (the sorted tokens
+ * and the partial sums of entries with many tokens).  Pure host arithmetic; 0
+ * for invalid sizes.
+ */
+size_t uattn_embedding_backward_workspace_bytes(int32_t num_tokens, int32_t hidden_dim);
+
+/*
+ * The gradient of the embedding table:
+ *
+ *   grad[v] = scale * sum over t with ids[t] = v of dout[t]   (+ grad[v] with accumulate)
+ *
+ *   dout        [num_tokens, dout_stride] bf16, first hidden_dim used
+ *   ids         [num_tokens] int32; ids outside [0, vocab) add nothing
+ *   grad        [vocab, grad_stride] bf16 (grad_fp32 0) or fp32 (grad_fp32 1),
+ *               first hidden_dim of every row written.  accumulate 0: rows no id
+ *               names become zeros; accumulate 1: they are left as they were
+ *   workspace   at least uattn_embedding_backward_workspace_bytes bytes, 16-byte
+ *               aligned, no initial contents needed; calls sharing a workspace must
+ *               be ordered on one stream
+ *   num_tokens at most 2^30 (UATTN_EUNSUPPORTED above); hidden_dim a multiple of
+ *   8; dout_stride a multiple of 8, grad_stride of 16 bytes; pointers 16-byte aligned.
+ *
+ * The tokens are sorted by id; an entry's rows are added in ascending order of t
+ * in fp32, 64 at a time, then these sums in order, with one rounding at the end:
+ * a row's bits depend on its own tokens alone, and repeated calls give the same.
+ */
+uattn_status uattn_embedding_backward(const void* dout, int64_t dout_stride, const int32_t* ids, float scale,
+                                      int32_t num_tokens, int32_t vocab, int32_t hidden_dim, void* grad,
+                                      int64_t grad_stride, int32_t grad_fp32, int32_t accumulate, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/*
+ * The logit processing between the LM head and the log-probability or the
+ * sampler (Section 3.1: one deterministic processing in both regimes): penalties
+ * for repeated tokens, biases, and a grammar's mask.  For every row t and entry
+ * v, x starting as logits[t][v]:
+ *
+ *   v among the row's history:              x = x > 0 ? x / repetition : x * repetition
+ *   n = times v occurs in its response:     x = x - frequency * n;  n > 0: x = x - presence
+ *   the row's biases name v:                x = x + the value of the last that does
+ *   the row's mask has no bit v:            x = -inf
+ *   out[t][v] = bf16(x)
+ *
+ * in fp32, rounded once.  A row's history is a range of `tokens`, so that a
+ * decode step (a sequence so far) and the update (the prefix of a position in a
+ * packed sequence) describe the same row and get the same bits.
+ *
+ *   logits       [num_rows, logits_stride] bf16, first vocab used
+ *   tokens       [num_tokens] int32, packed sequences; ids outside [0, vocab) are ignored
+ *   history      [num_rows, 3] int32: begin, start of the response, end of the
+ *                row's range of tokens (clamped to it), or NULL: no penalties
+ *   penalties    [num_rows, 3] fp32: repetition, frequency, presence (1, 0, 0 for
+ *                none); NULL together with history
+ *   bias_ids, bias_values   [num_bias] int32 and fp32; ids outside [0, vocab) are ignored
+ *   bias_rows    [num_rows, 2] int32: begin and end of the row's biases (clamped), or NULL
+ *   mask         [num_masks, mask_stride] 32-bit words, bit v % 32 of word v / 32
+ *                set where v is allowed; or NULL: no masks
+ *   mask_rows    [num_rows] int32, the mask of each row (outside [0, num_masks):
+ *                none), or NULL: row t has mask t, num_masks >= num_rows
+ *   out          [num_rows, out_stride] bf16, first vocab written (may be logits
+ *                itself, with the same stride)
+ *   strides      >= vocab and multiples of 8 (mask_stride >= ceil(vocab / 32) words);
+ *                logits and out 16-byte aligned
+ *
+ * A row whose mask allows nothing is -inf everywhere (uattn_logprob gives NaN for it).
+ */
+uattn_status uattn_logits_process(const void* logits, int64_t logits_stride, int32_t num_rows, int32_t vocab,
+                                  const int32_t* tokens, int32_t num_tokens, const int32_t* history,
+                                  const float* penalties, const int32_t* bias_ids, const float* bias_values,
+                                  int32_t num_bias, const int32_t* bias_rows, const uint32_t* mask,
+                                  int64_t mask_stride, int32_t num_masks, const int32_t* mask_rows, void* out,
+                                  int64_t out_stride, void* stream);
+
+/*
+ * The gradient of uattn_logits_process with respect to the logits:
+ *
+ *   dlogits = 0 where masked; elsewhere dout, and for entries of the history
+ *   logits > 0 ? dout / repetition : dout * repetition
+ *
+ *   dout      [num_rows, dout_stride] bf16, gradient of the processed logits
+ *   logits    the logits given to uattn_logits_process (read at entries of the history)
+ *   dlogits   [num_rows, dlogits_stride] bf16, first vocab written (may be dout
+ *             itself, with the same stride)
+ *   the others as there (biases, frequency and presence have no part in it)
+ */
+uattn_status uattn_logits_process_backward(const void* dout, int64_t dout_stride, const void* logits,
+                                           int64_t logits_stride, int32_t num_rows, int32_t vocab,
+                                           const int32_t* tokens, int32_t num_tokens, const int32_t* history,
+                                           const float* penalties, const uint32_t* mask, int64_t mask_stride,
+                                           int32_t num_masks, const int32_t* mask_rows, void* dlogits,
+                                           int64_t dlogits_stride, void* stream);
+
+/*
+ * The gradient of uattn_logprob with respect to the logits:
+ *
+ *   dlogits[t][v] = dlogp[t] * inv_temperature * (1[v = targets[t]] - p_v),
+ *   p = softmax(logits[t] * inv_temperature)
+ *
+ * in fp32, rounded once.
+ *
+ *   logits, row_stride, targets, vocab, inv_temperature   as passed to uattn_logprob
+ *              (inv_temperature * log2(e) finite too)
+ *   dlogp      [num_rows] fp32, gradient of the log-probabilities.  A row whose
+ *              dlogp is 0 (a padded or masked token) gets zeros whatever its
+ *              logits and target hold
+ *   dlogits    [num_rows, dlogits_stride] bf16, first vocab written; 16-byte
+ *              aligned, stride a multiple of 8; not logits itself
+ *
+ * A row whose target is outside [0, vocab), or whose logits are all -inf, gets
+ * NaN.  A row is computed by one workgroup in an order that depends only on vocab.
+ */
+uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, const int32_t* targets, const float* dlogp,
+                                    int32_t num_rows, int32_t vocab, float inv_temperature, void* dlogits,
+                                    int64_t dlogits_stride, void* stream);
 
 #ifdef __cplusplus
 }

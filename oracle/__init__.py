@@ -33,3 +33,6 @@ from .lm_head import abs_dot, lm_head_logprob_fp64, logits_bf16, logits_fp64  # 
 from .logprob import logprob_fp64  # noqa: F401
 from .norm_rope import qk_norm_rope, rms_norm_bf16, rope_neox, rope_table  # noqa: F401
 from .attention_backward import attention_backward_fp64, backward_error_scales, dq_rows_fp64  # noqa: F401
+from .embedding import embedding_backward_fp64, embedding_fp64  # noqa: F401
+from .logits import logits_process_backward_fp64, logits_process_fp64, logprob_backward_fp64  # noqa: F401
+from .residual_norm import residual_norm_backward_fp64, residual_norm_fp64  # noqa: F401

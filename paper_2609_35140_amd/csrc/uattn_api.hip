@@ -35,6 +35,73 @@ bool copy_back(std::vector<T>& host, const T* dev, size_t n) {
   return hipMemcpy(host.data(), dev, n * sizeof(T), hipMemcpyDeviceToHost) == hipSuccess;
 }
 
+bool is_finite(float x) { return x - x == 0.f; }
+
+// A device array copied back for UATTN_VALIDATE; host is nullptr where that fails.
+template <class T>
+struct Copied {
+  T* host;
+  Copied(const T* dev, size_t n) : host(static_cast<T*>(malloc(n > 0 ? n * sizeof(T) : 1))) {
+    if (host != nullptr && n > 0 && hipMemcpy(host, dev, n * sizeof(T), hipMemcpyDeviceToHost) != hipSuccess) {
+      free(host);
+      host = nullptr;
+    }
+  }
+  ~Copied() { free(host); }
+  Copied(const Copied&) = delete;
+  Copied& operator=(const Copied&) = delete;
+};
+
+bool all_below(const int32_t* dev, int32_t n, int32_t limit) {
+  Copied<int32_t> c(dev, static_cast<size_t>(n));
+  if (c.host == nullptr) return false;
+  for (int32_t i = 0; i < n; ++i)
+    if (c.host[i] >= limit) return false;
+  return true;
+}
+
+// Widths a row of the residual norm may have: 16-byte pieces, held by one workgroup's registers.
+bool norm_width_ok(int32_t hidden_dim) { return hidden_dim % 8 == 0 && hidden_dim <= 16384; }
+
+constexpr int32_t kMaxSortedTokens = 1 << 30;
+
+// Ranges [begin, end) of `width` columns: column 0 to the last ascending, inside [0, limit].
+bool ranges_ok(const int32_t* dev, int32_t rows, int width, int32_t limit) {
+  Copied<int32_t> c(dev, static_cast<size_t>(rows) * width);
+  if (c.host == nullptr) return false;
+  for (size_t r = 0; r < static_cast<size_t>(rows); ++r) {
+    int32_t least = 0;
+    for (int k = 0; k < width; ++k) {
+      const int32_t v = c.host[r * width + k];
+      if (v < least || v > limit) return false;
+      least = v;
+    }
+  }
+  return true;
+}
+
+// What the logit processing and its gradient ask of their common arguments.
+uattn_status check_logits(const uattn::LogitsLaunch& a) {
+  if (a.num_rows < 0 || a.vocab <= 0 || a.num_tokens < 0 || a.num_bias < 0 || a.num_masks < 0) return UATTN_EINVAL;
+  if (a.logits_stride < a.vocab || (a.logits_stride % 8) != 0 || a.out_stride < a.vocab || (a.out_stride % 8) != 0)
+    return UATTN_EINVAL;
+  if ((a.history == nullptr) != (a.penalties == nullptr)) return UATTN_EINVAL;
+  if (a.history != nullptr && a.num_tokens > 0 && a.tokens == nullptr) return UATTN_EINVAL;
+  if (a.bias_rows != nullptr && a.num_bias > 0 && (a.bias_ids == nullptr || a.bias_values == nullptr))
+    return UATTN_EINVAL;
+  if (a.mask != nullptr && a.mask_stride < (static_cast<int64_t>(a.vocab) + 31) / 32) return UATTN_EINVAL;
+  if (a.mask != nullptr && a.mask_rows == nullptr && a.num_masks < a.num_rows) return UATTN_EINVAL;
+  if (a.num_rows == 0) return UATTN_OK;
+  if (!a.logits || !a.out || !aligned16(a.logits) || !aligned16(a.out)) return UATTN_EINVAL;
+  if (validate_env()) {
+    if (a.history != nullptr && !ranges_ok(a.history, a.num_rows, 3, a.num_tokens)) return UATTN_EINVAL;
+    if (a.bias_rows != nullptr && !ranges_ok(a.bias_rows, a.num_rows, 2, a.num_bias)) return UATTN_EINVAL;
+    if (a.mask != nullptr && a.mask_rows != nullptr && !all_below(a.mask_rows, a.num_rows, a.num_masks))
+      return UATTN_EINVAL;
+  }
+  return UATTN_OK;
+}
+
 }  // namespace
 
 namespace uattn {
@@ -434,6 +501,234 @@ uattn_status uattn_prefill_backward(const void* q, const void* k, const void* v,
   a.c = exp2_scale(softmax_scale);
   a.scale = softmax_scale;
   return uattn::launch_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_residual_norm(const void* x, const void* post_weight, const void* gate, int64_t gate_stride,
+                                 float scale, const void* residual, const void* pre_weight, float eps,
+                                 int32_t num_tokens, int32_t hidden_dim, void* residual_out, void* y, void* stream) {
+  if (num_tokens < 0 || hidden_dim <= 0 || !is_finite(scale) || !(eps >= 0.f) || !is_finite(eps)) return UATTN_EINVAL;
+  if (!norm_width_ok(hidden_dim)) return UATTN_EUNSUPPORTED;
+  if (gate_stride != 0 && gate_stride != hidden_dim) return UATTN_EINVAL;
+  if (num_tokens == 0) return UATTN_OK;
+  if (!residual || (pre_weight == nullptr) != (y == nullptr) || (x == nullptr) != (residual_out == nullptr))
+    return UATTN_EINVAL;
+  if (x == nullptr && (post_weight != nullptr || gate != nullptr || y == nullptr)) return UATTN_EINVAL;
+  if (!aligned16(x) || !aligned16(post_weight) || !aligned16(gate) || !aligned16(residual) || !aligned16(pre_weight) ||
+      !aligned16(residual_out) || !aligned16(y))
+    return UATTN_EINVAL;
+  uattn::ResidualNormLaunch a;
+  a.x = x;
+  a.post_weight = post_weight;
+  a.gate = gate;
+  a.gate_stride = gate_stride;
+  a.scale = scale;
+  a.residual = residual;
+  a.pre_weight = pre_weight;
+  a.eps = eps;
+  a.num_tokens = num_tokens;
+  a.hidden_dim = hidden_dim;
+  a.residual_out = residual_out;
+  a.y = y;
+  return uattn::launch_residual_norm(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+size_t uattn_residual_norm_backward_workspace_bytes(int32_t num_tokens, int32_t hidden_dim) {
+  if (num_tokens <= 0 || hidden_dim <= 0 || !norm_width_ok(hidden_dim)) return 0;
+  return uattn::residual_norm_backward_ws_bytes(num_tokens, hidden_dim);
+}
+
+uattn_status uattn_residual_norm_backward(const void* dy, const void* dresidual_out, const void* residual_out,
+                                          const void* pre_weight, const void* x, const void* post_weight,
+                                          const void* gate, int64_t gate_stride, float scale, float eps,
+                                          int32_t num_tokens, int32_t hidden_dim, void* dresidual, void* dx,
+                                          float* dpre_weight, float* dpost_weight, void* dgate, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  if (num_tokens < 0 || hidden_dim <= 0 || !is_finite(scale) || !(eps >= 0.f) || !is_finite(eps)) return UATTN_EINVAL;
+  if (!norm_width_ok(hidden_dim)) return UATTN_EUNSUPPORTED;
+  if (gate_stride != 0 && gate_stride != hidden_dim) return UATTN_EINVAL;
+  // which gradients belong to which of the forward's parts, whatever the number of tokens
+  if ((pre_weight == nullptr) != (dpre_weight == nullptr) || (post_weight == nullptr) != (dpost_weight == nullptr) ||
+      (gate == nullptr) != (dgate == nullptr))
+    return UATTN_EINVAL;
+  if (num_tokens > 0) {
+    if (!dresidual || (dy == nullptr) != (pre_weight == nullptr)) return UATTN_EINVAL;
+    if (dy == nullptr && dresidual_out == nullptr) return UATTN_EINVAL;
+    if (dy != nullptr && residual_out == nullptr) return UATTN_EINVAL;
+    if ((post_weight != nullptr || gate != nullptr) && (x == nullptr || dx == nullptr)) return UATTN_EINVAL;
+  }
+  if (!aligned16(dy) || !aligned16(dresidual_out) || !aligned16(residual_out) || !aligned16(pre_weight) || !aligned16(x) ||
+      !aligned16(post_weight) || !aligned16(gate) || !aligned16(dresidual) || !aligned16(dx) || !aligned16(dpre_weight) ||
+      !aligned16(dpost_weight) || !aligned16(dgate))
+    return UATTN_EINVAL;
+  const size_t need = uattn_residual_norm_backward_workspace_bytes(num_tokens, hidden_dim);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return UATTN_EWORKSPACE;
+  uattn::ResidualNormBackwardLaunch a;
+  a.dy = dy;
+  a.dresidual_out = dresidual_out;
+  a.residual_out = residual_out;
+  a.pre_weight = pre_weight;
+  a.x = x;
+  a.post_weight = post_weight;
+  a.gate = gate;
+  a.gate_stride = gate_stride;
+  a.scale = scale;
+  a.eps = eps;
+  a.num_tokens = num_tokens;
+  a.hidden_dim = hidden_dim;
+  a.dresidual = dresidual;
+  a.dx = dx;
+  a.dpre_weight = dpre_weight;
+  a.dpost_weight = dpost_weight;
+  a.dgate = dgate;
+  a.workspace = workspace;
+  return uattn::launch_residual_norm_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK
+                                                                                                 : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_embedding(const int32_t* ids, const void* table, int64_t table_stride, float scale,
+                             int32_t num_tokens, int32_t vocab, int32_t hidden_dim, void* out, int64_t out_stride,
+                             void* stream) {
+  if (num_tokens < 0 || vocab <= 0 || hidden_dim <= 0 || (hidden_dim % 8) != 0 || !is_finite(scale)) return UATTN_EINVAL;
+  if (table_stride < hidden_dim || out_stride < hidden_dim || (table_stride % 8) != 0 || (out_stride % 8) != 0)
+    return UATTN_EINVAL;
+  if (num_tokens == 0) return UATTN_OK;
+  if (!ids || !table || !out || !aligned16(table) || !aligned16(out)) return UATTN_EINVAL;
+  if (validate_env() && !all_below(ids, num_tokens, vocab)) return UATTN_EINVAL;
+  uattn::EmbeddingLaunch a;
+  a.ids = ids;
+  a.table = table;
+  a.table_stride = table_stride;
+  a.scale = scale;
+  a.num_tokens = num_tokens;
+  a.vocab = vocab;
+  a.hidden_dim = hidden_dim;
+  a.out = out;
+  a.out_stride = out_stride;
+  return uattn::launch_embedding(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+size_t uattn_embedding_backward_workspace_bytes(int32_t num_tokens, int32_t hidden_dim) {
+  if (num_tokens <= 0 || hidden_dim <= 0 || num_tokens > kMaxSortedTokens) return 0;
+  return uattn::embedding_backward_ws_bytes(num_tokens, hidden_dim);
+}
+
+uattn_status uattn_embedding_backward(const void* dout, int64_t dout_stride, const int32_t* ids, float scale,
+                                      int32_t num_tokens, int32_t vocab, int32_t hidden_dim, void* grad,
+                                      int64_t grad_stride, int32_t grad_fp32, int32_t accumulate, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  if (num_tokens < 0 || vocab <= 0 || hidden_dim <= 0 || (hidden_dim % 8) != 0 || !is_finite(scale)) return UATTN_EINVAL;
+  if ((grad_fp32 & ~1) != 0 || (accumulate & ~1) != 0) return UATTN_EINVAL;
+  if (grad_stride < hidden_dim || (grad_stride % (grad_fp32 ? 4 : 8)) != 0) return UATTN_EINVAL;
+  if (dout_stride < hidden_dim || (dout_stride % 8) != 0) return UATTN_EINVAL;
+  if (num_tokens > kMaxSortedTokens) return UATTN_EUNSUPPORTED;
+  if (num_tokens == 0 && accumulate) return UATTN_OK;
+  if (!grad || !aligned16(grad)) return UATTN_EINVAL;
+  if (num_tokens > 0 && (!dout || !ids || !aligned16(dout))) return UATTN_EINVAL;
+  const size_t need = uattn_embedding_backward_workspace_bytes(num_tokens, hidden_dim);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return UATTN_EWORKSPACE;
+  if (validate_env() && !all_below(ids, num_tokens, vocab)) return UATTN_EINVAL;
+  uattn::EmbeddingBackwardLaunch a;
+  a.dout = dout;
+  a.dout_stride = dout_stride;
+  a.ids = ids;
+  a.scale = scale;
+  a.num_tokens = num_tokens;
+  a.vocab = vocab;
+  a.hidden_dim = hidden_dim;
+  a.grad = grad;
+  a.grad_stride = grad_stride;
+  a.grad_fp32 = grad_fp32 != 0;
+  a.accumulate = accumulate != 0;
+  a.workspace = workspace;
+  return uattn::launch_embedding_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_logits_process(const void* logits, int64_t logits_stride, int32_t num_rows, int32_t vocab,
+                                  const int32_t* tokens, int32_t num_tokens, const int32_t* history,
+                                  const float* penalties, const int32_t* bias_ids, const float* bias_values,
+                                  int32_t num_bias, const int32_t* bias_rows, const uint32_t* mask,
+                                  int64_t mask_stride, int32_t num_masks, const int32_t* mask_rows, void* out,
+                                  int64_t out_stride, void* stream) {
+  uattn::LogitsLaunch a{};
+  a.logits = logits;
+  a.logits_stride = logits_stride;
+  a.num_rows = num_rows;
+  a.vocab = vocab;
+  a.tokens = tokens;
+  a.num_tokens = num_tokens;
+  a.history = history;
+  a.penalties = penalties;
+  a.bias_ids = bias_ids;
+  a.bias_values = bias_values;
+  a.num_bias = num_bias;
+  a.bias_rows = bias_rows;
+  a.mask = mask;
+  a.mask_stride = mask_stride;
+  a.num_masks = num_masks;
+  a.mask_rows = mask_rows;
+  a.out = out;
+  a.out_stride = out_stride;
+  const uattn_status st = check_logits(a);
+  if (st != UATTN_OK || num_rows == 0) return st;
+  return uattn::launch_logits_process(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_logits_process_backward(const void* dout, int64_t dout_stride, const void* logits,
+                                           int64_t logits_stride, int32_t num_rows, int32_t vocab,
+                                           const int32_t* tokens, int32_t num_tokens, const int32_t* history,
+                                           const float* penalties, const uint32_t* mask, int64_t mask_stride,
+                                           int32_t num_masks, const int32_t* mask_rows, void* dlogits,
+                                           int64_t dlogits_stride, void* stream) {
+  uattn::LogitsLaunch a{};
+  a.dout = dout;
+  a.dout_stride = dout_stride;
+  a.logits = logits;
+  a.logits_stride = logits_stride;
+  a.num_rows = num_rows;
+  a.vocab = vocab;
+  a.tokens = tokens;
+  a.num_tokens = num_tokens;
+  a.history = history;
+  a.penalties = penalties;
+  a.mask = mask;
+  a.mask_stride = mask_stride;
+  a.num_masks = num_masks;
+  a.mask_rows = mask_rows;
+  a.out = dlogits;
+  a.out_stride = dlogits_stride;
+  const uattn_status st = check_logits(a);
+  if (st != UATTN_OK || num_rows == 0) return st;
+  if (!dout || !aligned16(dout) || dout_stride < vocab || (dout_stride % 8) != 0) return UATTN_EINVAL;
+  return uattn::launch_logits_process_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK
+                                                                                                  : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, const int32_t* targets, const float* dlogp,
+                                    int32_t num_rows, int32_t vocab, float inv_temperature, void* dlogits,
+                                    int64_t dlogits_stride, void* stream) {
+  if (num_rows < 0 || vocab <= 0 || row_stride < vocab || (row_stride % 8) != 0) return UATTN_EINVAL;
+  if (dlogits_stride < vocab || (dlogits_stride % 8) != 0) return UATTN_EINVAL;
+  // the exponent's factor, inv_temperature * log2(e), has to be finite too
+  if (!scale_ok(inv_temperature) || !scale_ok(exp2_scale(inv_temperature))) return UATTN_EINVAL;
+  if (num_rows == 0) return UATTN_OK;
+  if (!logits || !targets || !dlogp || !dlogits || !aligned16(logits) || !aligned16(dlogits)) return UATTN_EINVAL;
+  if (validate_env()) {
+    Copied<int32_t> tg(targets, num_rows);
+    if (tg.host == nullptr) return UATTN_EINVAL;
+    for (int32_t t = 0; t < num_rows; ++t)
+      if (tg.host[t] < 0 || tg.host[t] >= vocab) return UATTN_EINVAL;
+  }
+  uattn::LogprobBackwardLaunch a;
+  a.logits = logits;
+  a.row_stride = row_stride;
+  a.targets = targets;
+  a.dlogp = dlogp;
+  a.num_rows = num_rows;
+  a.vocab = vocab;
+  a.inv_temperature = inv_temperature;
+  a.dlogits = dlogits;
+  a.dlogits_stride = dlogits_stride;
+  return uattn::launch_logprob_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
 
 }  // extern "C"

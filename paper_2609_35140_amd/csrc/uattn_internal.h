@@ -126,6 +126,109 @@ struct BackwardLaunch {
 hipError_t launch_backward(const BackwardLaunch& a, hipStream_t stream);
 size_t backward_ws_bytes(int64_t total_tokens, int64_t num_q_heads);
 
+struct ResidualNormLaunch {
+  const void* x;            // nullptr: no block output, the residual is normalized as it is
+  const void* post_weight;  // nullptr: x is not normalized
+  const void* gate;         // nullptr, one row (gate_stride 0) or a row per token
+  int64_t gate_stride;
+  float scale;
+  const void* residual;
+  const void* pre_weight;   // nullptr with y
+  float eps;
+  int32_t num_tokens, hidden_dim;
+  void* residual_out;       // nullptr with x
+  void* y;
+};
+
+hipError_t launch_residual_norm(const ResidualNormLaunch& a, hipStream_t stream);
+
+struct ResidualNormBackwardLaunch {
+  const void* dy;             // nullptr with pre_weight and dpre_weight
+  const void* dresidual_out;  // nullptr: zeros
+  const void* residual_out;
+  const void* pre_weight;
+  const void* x;              // nullptr where neither post_weight nor gate is given
+  const void* post_weight;
+  const void* gate;
+  int64_t gate_stride;
+  float scale, eps;
+  int32_t num_tokens, hidden_dim;
+  void* dresidual;
+  void* dx;                   // nullptr: no block output
+  float* dpre_weight;
+  float* dpost_weight;
+  void* dgate;                // fp32 row (gate_stride 0) or bf16 rows
+  void* workspace;            // residual_norm_backward_ws_bytes(num_tokens, hidden_dim)
+};
+
+hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hipStream_t stream);
+size_t residual_norm_backward_ws_bytes(int64_t num_tokens, int64_t hidden_dim);
+
+struct EmbeddingLaunch {
+  const int32_t* ids;
+  const void* table;
+  int64_t table_stride;
+  float scale;
+  int32_t num_tokens, vocab, hidden_dim;
+  void* out;
+  int64_t out_stride;
+};
+
+hipError_t launch_embedding(const EmbeddingLaunch& a, hipStream_t stream);
+
+struct EmbeddingBackwardLaunch {
+  const void* dout;
+  int64_t dout_stride;
+  const int32_t* ids;
+  float scale;
+  int32_t num_tokens, vocab, hidden_dim;
+  void* grad;
+  int64_t grad_stride;
+  bool grad_fp32, accumulate;
+  void* workspace;  // embedding_backward_ws_bytes(num_tokens, hidden_dim)
+};
+
+hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream_t stream);
+size_t embedding_backward_ws_bytes(int64_t num_tokens, int64_t hidden_dim);
+
+struct LogitsLaunch {
+  const void* dout;  // backward only
+  int64_t dout_stride;
+  const void* logits;
+  int64_t logits_stride;
+  int32_t num_rows, vocab;
+  const int32_t* tokens;
+  int32_t num_tokens;
+  const int32_t* history;    // nullptr: no penalties
+  const float* penalties;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int32_t num_bias;
+  const int32_t* bias_rows;  // nullptr: no biases
+  const uint32_t* mask;      // nullptr: no mask
+  int64_t mask_stride;
+  int32_t num_masks;
+  const int32_t* mask_rows;
+  void* out;
+  int64_t out_stride;
+};
+
+hipError_t launch_logits_process(const LogitsLaunch& a, hipStream_t stream);
+hipError_t launch_logits_process_backward(const LogitsLaunch& a, hipStream_t stream);
+
+struct LogprobBackwardLaunch {
+  const void* logits;
+  int64_t row_stride;
+  const int32_t* targets;
+  const float* dlogp;
+  int32_t num_rows, vocab;
+  float inv_temperature;
+  void* dlogits;
+  int64_t dlogits_stride;
+};
+
+hipError_t launch_logprob_backward(const LogprobBackwardLaunch& a, hipStream_t stream);
+
 // A grid holds fewer than 2^32 threads: past that it starts modulo 2^32, the rest
 // is never run and no error is reported.  Calls launch(first, n) for consecutive
 // runs of workgroups that fit, each cut at a multiple of the XCD count.

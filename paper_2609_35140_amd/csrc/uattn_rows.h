@@ -1,0 +1,81 @@
+// Shared by the row-wise kernels: 16-byte pieces of bf16 rows, and sums over a
+// wave or a workgroup in an order fixed by the thread count alone.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#pragma clang fp contract(off)
+
+namespace uattn {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Two values rounded to bf16 (nearest even) by one instruction.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// Eight bf16 values of a 16-byte piece, and back.
+__device__ __forceinline__ void unpack8(const u32x4& w, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = bf16_lo(w[j]);
+    x[2 * j + 1] = bf16_hi(w[j]);
+  }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+  return w;
+}
+
+__device__ __forceinline__ u32x4 load16(const void* p, int64_t piece) {
+  return reinterpret_cast<const u32x4*>(p)[piece];
+}
+__device__ __forceinline__ void store16(void* p, int64_t piece, const u32x4& w) {
+  reinterpret_cast<u32x4*>(p)[piece] = w;
+}
+
+// DPP: every lane reads another of its 16; all lanes of the patterns used have a source.
+template <int ctrl>
+__device__ __forceinline__ float dpp_read(float x) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), ctrl, 0xF, 0xF, true));
+}
+
+// The sum over the wave's 64 lanes in every lane, the same bits in all of them: rotations inside 16
+// lanes (after the distances 8 and 4 the sums repeat with period 4, so a swap is an xor), then the
+// two lane swaps, whose operands come in the same order in both halves.
+__device__ __forceinline__ float wave_sum(float x) {
+  x = x + dpp_read<0x128>(x);  // row_ror:8
+  x = x + dpp_read<0x124>(x);  // row_ror:4
+  x = x + dpp_read<0x4E>(x);   // lane ^ 2
+  x = x + dpp_read<0xB1>(x);   // lane ^ 1
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// The sum over a workgroup of kWaves waves, in every thread: wave sums through `slots`, added in
+// wave order.  Calls in a row take different slots (one barrier each), so that a wave that is ahead
+// does not overwrite what another still reads.
+template <int kWaves>
+__device__ __forceinline__ float block_sum(float x, float* slots) {
+  x = wave_sum(x);
+  if constexpr (kWaves == 1) return x;
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = x;
+  __syncthreads();
+  float s = slots[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) s = s + slots[w];
+  return s;
+}
+
+}  // namespace uattn

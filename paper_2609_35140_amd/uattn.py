@@ -7,6 +7,7 @@ PyTorch fallback -- if the library is missing, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -72,6 +73,28 @@ def _load():
     lib.uattn_kv_write.restype = c_i32
     lib.uattn_kv_write.argtypes = [c_p, c_p, c_i64, c_p, c_p, c_p, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
                                    c_p, c_p, c_p]
+    lib.uattn_residual_norm.restype = c_i32
+    lib.uattn_residual_norm.argtypes = [c_p, c_p, c_p, c_i64, c_f, c_p, c_p, c_f, c_i32, c_i32, c_p, c_p, c_p]
+    lib.uattn_residual_norm_backward_workspace_bytes.restype = c_sz
+    lib.uattn_residual_norm_backward_workspace_bytes.argtypes = [c_i32, c_i32]
+    lib.uattn_residual_norm_backward.restype = c_i32
+    lib.uattn_residual_norm_backward.argtypes = [c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_i64, c_f, c_f, c_i32, c_i32, c_p,
+                                                 c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
+    lib.uattn_embedding.restype = c_i32
+    lib.uattn_embedding.argtypes = [c_p, c_p, c_i64, c_f, c_i32, c_i32, c_i32, c_p, c_i64, c_p]
+    lib.uattn_embedding_backward_workspace_bytes.restype = c_sz
+    lib.uattn_embedding_backward_workspace_bytes.argtypes = [c_i32, c_i32]
+    lib.uattn_embedding_backward.restype = c_i32
+    lib.uattn_embedding_backward.argtypes = [c_p, c_i64, c_p, c_f, c_i32, c_i32, c_i32, c_p, c_i64, c_i32, c_i32, c_p,
+                                             c_sz, c_p]
+    lib.uattn_logits_process.restype = c_i32
+    lib.uattn_logits_process.argtypes = [c_p, c_i64, c_i32, c_i32, c_p, c_i32, c_p, c_p, c_p, c_p, c_i32, c_p, c_p,
+                                         c_i64, c_i32, c_p, c_p, c_i64, c_p]
+    lib.uattn_logits_process_backward.restype = c_i32
+    lib.uattn_logits_process_backward.argtypes = [c_p, c_i64, c_p, c_i64, c_i32, c_i32, c_p, c_i32, c_p, c_p, c_p,
+                                                  c_i64, c_i32, c_p, c_p, c_i64, c_p]
+    lib.uattn_logprob_backward.restype = c_i32
+    lib.uattn_logprob_backward.argtypes = [c_p, c_i64, c_p, c_p, c_i32, c_i32, c_f, c_p, c_i64, c_p]
     _lib = lib
     return lib
 
@@ -494,6 +517,328 @@ def lm_head_logprob(hidden, weight, targets, inv_temperature: float = 1.0, out=N
                                          T, V, H, float(inv_temperature), _ptr(out), _ptr(logits),
                                          logits.stride(0) if logits is not None else 0, _ptr(workspace),
                                          workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+# The row-wise operators below put their outputs and workspaces on the stream the
+# call runs on (torch's allocator reuses memory in a stream's order), and run on
+# their tensors' device where another one is current.
+_HERE = contextlib.nullcontext()
+
+
+def _place(device: int, stream):
+    import torch
+    if stream is not None:
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        return torch.cuda.stream(stream)
+    return _HERE if device == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _one_device(*tensors) -> int:
+    """The GPU that holds all the tensors (None among them is skipped)."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on one GPU")
+    return device
+
+
+def _f32_cuda(t, name):
+    import torch
+    if not (t.dtype == torch.float32 and t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous float32 on the GPU")
+
+
+def _shaped(t, shape, name):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be of shape {shape}")
+
+
+def _out_rows(out, rows, width, like):
+    """``out``, or new bf16 rows whose starts are 16-byte aligned."""
+    import torch
+    if out is None:
+        return torch.empty((rows, (width + 7) // 8 * 8), dtype=torch.bfloat16, device=like.device)[:, :width]
+    _bf16_rows(out, "out")
+    _shaped(out, (rows, width), "out")
+    return out
+
+
+def _row_stride(t) -> int:
+    """Elements from row to row of a 2-D tensor (any would do for one row: torch may report what the call refuses)."""
+    return t.stride(0) if t.shape[0] > 1 else max((t.shape[1] + 7) // 8 * 8, t.stride(0) // 8 * 8)
+
+
+def _norm_parts(residual, x, post_weight, gate, pre_weight):
+    """Checks of the residual norm's forward inputs; returns (tokens, width, gate's row stride)."""
+    _bf16_cuda(residual, "residual")
+    _need(residual.dim() == 2, "residual must be [T, H]")
+    T, H = residual.shape
+    gate_stride = 0
+    if x is not None:
+        _bf16_cuda(x, "x")
+        _shaped(x, (T, H), "x")
+    for name, w in (("post_weight", post_weight), ("pre_weight", pre_weight)):
+        if w is not None:
+            _bf16_cuda(w, name)
+            _shaped(w, (H,), name)
+    if gate is not None:
+        _bf16_cuda(gate, "gate")
+        _need(tuple(gate.shape) in ((H,), (T, H)), "gate must be [H] or [T, H]")
+        gate_stride = H if gate.dim() == 2 else 0
+    return T, H, gate_stride
+
+
+def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6,
+                  residual_out=None, y=None, stream=None):
+    """The norms behind a block and before the next with the residual sum between them (uattn_residual_norm).
+
+      u = x * r(x) * post_weight;  s = residual + scale * gate * u;  y = s * r(s) * pre_weight
+
+      residual, x [T, H] bf16; post_weight, pre_weight [H] bf16; gate [H] or [T, H] bf16.
+      Every part but residual may be left out, not x and pre_weight both.  Returns
+      (residual_out, y): residual itself where there is no x, and None where there
+      is no pre_weight.  residual_out may be residual, y may be x (in place).
+    """
+    import torch
+    T, H, gate_stride = _norm_parts(residual, x, post_weight, gate, pre_weight)
+    _need(x is not None or pre_weight is not None, "x or pre_weight must be given")
+    _need(x is not None or (post_weight is None and gate is None and residual_out is None),
+          "post_weight, gate and residual_out belong to x")
+    _need(pre_weight is not None or y is None, "y belongs to pre_weight")
+    for name, t in (("residual_out", residual_out), ("y", y)):
+        if t is not None:
+            _bf16_cuda(t, name)
+            _shaped(t, (T, H), name)
+    with _place(_one_device(residual, x, post_weight, gate, pre_weight, residual_out, y), stream):
+        if x is not None and residual_out is None:
+            residual_out = torch.empty_like(residual)
+        if pre_weight is not None and y is None:
+            y = torch.empty_like(residual)
+        _check(_load().uattn_residual_norm(_ptr(x), _ptr(post_weight), _ptr(gate), gate_stride, scale, _ptr(residual),
+                                           _ptr(pre_weight), eps, T, H, _ptr(residual_out), _ptr(y), _stream(None)))
+    return (residual if x is None else residual_out), y
+
+
+def residual_norm_backward_workspace_bytes(num_tokens: int, hidden_dim: int) -> int:
+    return int(_load().uattn_residual_norm_backward_workspace_bytes(int(num_tokens), int(hidden_dim)))
+
+
+def _workspace(workspace, need: int, device):
+    import torch
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)  # no initial contents needed
+    _need(workspace.is_cuda and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
+    return workspace
+
+
+def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=None, post_weight=None, gate=None,
+                           scale: float = 1.0, eps: float = 1e-6, dresidual=None, dx=None, has_block: Optional[bool] = None,
+                           workspace=None, stream=None):
+    """Gradients of residual_norm (uattn_residual_norm_backward).
+
+      dy [T, H] bf16, gradient of y (None without pre_weight); dresidual_out [T, H]
+      bf16, gradient of residual_out (None: zeros); residual_out as the forward
+      returned it; x, post_weight, gate, scale, eps as passed to it.  has_block:
+      whether the forward had an x (by default, whether x is given here: where it
+      had neither post_weight nor gate, x itself is not read and need not be kept).
+      Returns (dresidual, dx, dpre_weight, dpost_weight, dgate): bf16 rows, fp32
+      [H] weight gradients, dgate fp32 [H] or bf16 [T, H] as the gate is; None for
+      what the forward did not have.
+    """
+    import torch
+    T, H, gate_stride = _norm_parts(residual_out, x, post_weight, gate, pre_weight)
+    if has_block is None:
+        has_block = x is not None
+    _need(has_block or (post_weight is None and gate is None and x is None and dx is None),
+          "x, post_weight, gate and dx belong to a forward with a block's output")
+    _need(x is not None or (post_weight is None and gate is None), "the gradients of post_weight and gate need x")
+    _need((dy is None) == (pre_weight is None), "dy and pre_weight belong together")
+    _need(dy is not None or dresidual_out is not None, "dy or dresidual_out must be given")
+    for name, t in (("dy", dy), ("dresidual_out", dresidual_out), ("dresidual", dresidual), ("dx", dx)):
+        if t is not None:
+            _bf16_cuda(t, name)
+            _shaped(t, (T, H), name)
+    dpre = dpost = dgate = None
+    device = residual_out.device
+    with _place(_one_device(residual_out, dy, dresidual_out, x, post_weight, gate, pre_weight, dresidual, dx, workspace), stream):
+        if dresidual is None:
+            dresidual = torch.empty_like(residual_out)
+        if has_block and dx is None:
+            dx = torch.empty_like(residual_out)
+        if pre_weight is not None:
+            dpre = torch.empty(H, dtype=torch.float32, device=device)
+        if post_weight is not None:
+            dpost = torch.empty(H, dtype=torch.float32, device=device)
+        if gate is not None:
+            dgate = torch.empty_like(gate) if gate_stride else torch.empty(H, dtype=torch.float32, device=device)
+        workspace = _workspace(workspace, residual_norm_backward_workspace_bytes(T, H), device)
+        _check(_load().uattn_residual_norm_backward(
+            _ptr(dy), _ptr(dresidual_out), _ptr(residual_out), _ptr(pre_weight), _ptr(x), _ptr(post_weight), _ptr(gate),
+            gate_stride, scale, eps, T, H, _ptr(dresidual), _ptr(dx), _ptr(dpre), _ptr(dpost), _ptr(dgate),
+            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(None)))
+    return dresidual, dx, dpre, dpost, dgate
+
+
+def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
+    """Rows of the embedding table, scaled (uattn_embedding).
+
+      ids [T] int32 (negative: padding, a row of zeros); table [V, H] bf16 (rows may be strided); returns [T, H] bf16.
+    """
+    _i32_cuda(ids, "ids")
+    _bf16_rows(table, "table")
+    _need(ids.dim() == 1, "ids must be [T]")
+    T, (V, H) = ids.shape[0], table.shape
+    with _place(_one_device(ids, table, out), stream):
+        out = _out_rows(out, T, H, table)
+        _check(_load().uattn_embedding(_ptr(ids), _ptr(table), _row_stride(table), scale, T, V, H, _ptr(out),
+                                       _row_stride(out), _stream(None)))
+    return out
+
+
+def embedding_backward_workspace_bytes(num_tokens: int, hidden_dim: int) -> int:
+    return int(_load().uattn_embedding_backward_workspace_bytes(int(num_tokens), int(hidden_dim)))
+
+
+def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, accumulate: bool = False, dtype=None,
+                       workspace=None, stream=None):
+    """The embedding table's gradient (uattn_embedding_backward).
+
+      dout [T, H] bf16 (rows may be strided); ids [T] int32.  Returns grad [V, H],
+      of ``dtype`` (bfloat16, or float32 by default) where none is given.  With
+      ``accumulate`` the sums are added to ``grad``, whose other rows stay as they
+      are; without, those rows become zeros.
+    """
+    import torch
+    _bf16_rows(dout, "dout")
+    _i32_cuda(ids, "ids")
+    T, H = dout.shape
+    _need(ids.shape == (T,), "ids must be [T]")
+    vocab = int(vocab)
+    if grad is None:
+        _need(not accumulate, "accumulate needs grad")
+        dtype = torch.float32 if dtype is None else dtype
+    else:
+        _need(dtype is None or dtype == grad.dtype, "grad is of another dtype")
+        dtype = grad.dtype
+        _need(grad.is_cuda and grad.dim() == 2 and grad.stride(1) == 1, "grad must be a 2-D GPU tensor with contiguous rows")
+        _shaped(grad, (vocab, H), "grad")
+    _need(dtype in (torch.float32, torch.bfloat16), "grad must be float32 or bfloat16")
+    with _place(_one_device(dout, ids, grad, workspace), stream):
+        if grad is None:
+            grad = torch.empty((vocab, H), dtype=dtype, device=dout.device)
+        workspace = _workspace(workspace, embedding_backward_workspace_bytes(T, H), dout.device)
+        _check(_load().uattn_embedding_backward(
+            _ptr(dout), _row_stride(dout), _ptr(ids), scale, T, vocab, H, _ptr(grad), _row_stride(grad),
+            int(dtype == torch.float32), int(bool(accumulate)), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream(None)))
+    return grad
+
+
+def _penalty_parts(rows, tokens, history, penalties):
+    _need((history is None) == (penalties is None) and (history is None) == (tokens is None),
+          "tokens, history and penalties belong together")
+    if history is None:
+        return 0
+    _i32_cuda(tokens, "tokens")
+    _i32_cuda(history, "history")
+    _f32_cuda(penalties, "penalties")
+    _need(tokens.dim() == 1, "tokens must be 1-D")
+    _shaped(history, (rows, 3), "history")
+    _shaped(penalties, (rows, 3), "penalties")
+    return tokens.shape[0]
+
+
+def _mask_parts(rows, vocab, mask, mask_rows):
+    """(masks, words from mask to mask)"""
+    _need(mask is not None or mask_rows is None, "mask_rows belongs to mask")
+    if mask is None:
+        return 0, 0
+    import torch
+    _need(mask.is_cuda and mask.dtype == torch.int32 and mask.dim() == 2 and mask.stride(1) == 1,
+          "mask must be a 2-D int32 GPU tensor with contiguous rows")
+    _need(mask.shape[1] >= (vocab + 31) // 32, "mask must have a bit for every vocabulary entry")
+    if mask_rows is None:
+        _need(mask.shape[0] >= rows, "mask needs a row for every row of logits, or mask_rows")
+    else:
+        _i32_cuda(mask_rows, "mask_rows")
+        _shaped(mask_rows, (rows,), "mask_rows")
+    return mask.shape[0], mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
+
+
+def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=None, bias_values=None, bias_rows=None,
+                   mask=None, mask_rows=None, out=None, stream=None):
+    """Penalties for repeated tokens, biases and grammar masks (uattn_logits_process).
+
+      logits [T, V] bf16 (rows may be strided); tokens [N] int32, packed sequences;
+      history [T, 3] int32 (begin, start of the response, end) and penalties [T, 3]
+      fp32 (repetition, frequency, presence) of every row; bias_ids [M] int32,
+      bias_values [M] fp32, bias_rows [T, 2] int32 (begin, end); mask [K, >= V/32]
+      int32 words (a set bit allows), mask_rows [T] int32 (negative: no mask).
+      Returns bf16 [T, V]; out may be logits (in place).
+    """
+    _bf16_rows(logits, "logits")
+    T, V = logits.shape
+    num_tokens = _penalty_parts(T, tokens, history, penalties)
+    num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows)
+    num_bias = 0
+    _need((bias_rows is None) == (bias_ids is None) and (bias_rows is None) == (bias_values is None),
+          "bias_ids, bias_values and bias_rows belong together")
+    if bias_rows is not None:
+        _i32_cuda(bias_ids, "bias_ids")
+        _f32_cuda(bias_values, "bias_values")
+        _i32_cuda(bias_rows, "bias_rows")
+        _need(bias_ids.dim() == 1 and bias_values.shape == bias_ids.shape, "bias_ids and bias_values must be [M]")
+        _shaped(bias_rows, (T, 2), "bias_rows")
+        num_bias = bias_ids.shape[0]
+    with _place(_one_device(logits, tokens, history, penalties, bias_ids, bias_values, bias_rows, mask, mask_rows, out), stream):
+        out = _out_rows(out, T, V, logits)
+        _check(_load().uattn_logits_process(
+            _ptr(logits), _row_stride(logits), T, V, _ptr(tokens), num_tokens, _ptr(history), _ptr(penalties),
+            _ptr(bias_ids), _ptr(bias_values), num_bias, _ptr(bias_rows), _ptr(mask), mask_stride, num_masks,
+            _ptr(mask_rows), _ptr(out), _row_stride(out), _stream(None)))
+    return out
+
+
+def logits_process_backward(dout, logits, tokens=None, history=None, penalties=None, mask=None, mask_rows=None, out=None,
+                            stream=None):
+    """Gradient of logits_process with respect to the logits (uattn_logits_process_backward).
+
+      dout [T, V] bf16, gradient of the processed logits; the others as passed to
+      logits_process.  Returns bf16 [T, V]; out may be dout (in place).
+    """
+    _bf16_rows(dout, "dout")
+    _bf16_rows(logits, "logits")
+    T, V = logits.shape
+    _shaped(dout, (T, V), "dout")
+    num_tokens = _penalty_parts(T, tokens, history, penalties)
+    num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows)
+    with _place(_one_device(dout, logits, tokens, history, penalties, mask, mask_rows, out), stream):
+        out = _out_rows(out, T, V, logits)
+        _check(_load().uattn_logits_process_backward(
+            _ptr(dout), _row_stride(dout), _ptr(logits), _row_stride(logits), T, V, _ptr(tokens), num_tokens,
+            _ptr(history), _ptr(penalties), _ptr(mask), mask_stride, num_masks, _ptr(mask_rows), _ptr(out),
+            _row_stride(out), _stream(None)))
+    return out
+
+
+def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=None, stream=None):
+    """Gradient of logprob with respect to the logits (uattn_logprob_backward).
+
+      logits [T, V] bf16 and targets [T] int32 as passed to logprob; dlogp [T] fp32
+      (0: the row gets zeros).  Returns bf16 [T, V].
+    """
+    _bf16_rows(logits, "logits")
+    T, V = logits.shape
+    _i32_cuda(targets, "targets")
+    _f32_cuda(dlogp, "dlogp")
+    _shaped(targets, (T,), "targets")
+    _shaped(dlogp, (T,), "dlogp")
+    with _place(_one_device(logits, targets, dlogp, out), stream):
+        out = _out_rows(out, T, V, logits)
+        _check(_load().uattn_logprob_backward(_ptr(logits), _row_stride(logits), _ptr(targets), _ptr(dlogp), T, V,
+                                              inv_temperature, _ptr(out), _row_stride(out), _stream(None)))
     return out
 
 

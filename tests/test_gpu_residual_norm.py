@@ -1,0 +1,258 @@
+"""GPU residual norm and its gradients against the float64 oracle, and what a row's bits may not depend on."""
+import numpy as np
+import pytest
+
+import oracle
+from paper_2609_35140_amd import inputs
+
+pytestmark = pytest.mark.gpu
+gu = pytest.importorskip("gpu_util")
+
+U = 2.0 ** -24   # one fp32 rounding
+HALF = 2.0 ** -8  # one bf16 rounding
+
+
+@pytest.fixture(scope="module")
+def ua():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_35140_amd import uattn
+    uattn.lib()
+    return uattn
+
+
+SHAPES = [(1, 8), (3, 64), (257, 120), (300, 512), (5, 1000), (700, 1024), (41, 2048), (9, 2056), (33, 4096), (1, 4096),
+          (600, 5120), (9, 8192), (2, 12008), (3, 16384)]
+FORMS = [  # block, post, gate, pre
+    (True, True, "shared", True), (True, True, "token", True), (True, False, "none", True), (True, False, "shared", True),
+    (True, True, "none", False), (False, False, "none", True), (True, False, "token", False), (True, False, "none", False)]
+
+
+def _case(T, H, form, seed=0, scale=0.5, eps=1e-6):
+    """Device tensors, the same in float64, and scale and eps."""
+    block, post, gate, pre = form
+    mk = lambda tag, shape, sigma=1.0: inputs.normal_bf16(shape, sigma, 300 + tag, T, H, seed)  # noqa: E731
+    bits = {"residual": mk(0, (T, H), 2.0), "pre": mk(1, (H,)) if pre else None, "x": mk(2, (T, H)) if block else None,
+            "post": mk(3, (H,)) if post else None,
+            "gate": None if gate == "none" else mk(4, (H,) if gate == "shared" else (T, H)),
+            "dy": mk(5, (T, H)) if pre else None, "dres": mk(6, (T, H)) if block or not pre else None}
+    dev = {k: None if b is None else gu.dev(b) for k, b in bits.items()}
+    ref = {k: None if b is None else oracle.bf16_to_f64(b) for k, b in bits.items()}
+    return dev, ref, dict(scale=scale, eps=eps)
+
+
+def _forward(ua, d, k, **kw):
+    return ua.residual_norm(d["residual"], d["pre"], x=d["x"], post_weight=d["post"], gate=d["gate"], **k, **kw)
+
+
+def _backward(ua, d, k, h, **kw):
+    return ua.residual_norm_backward(d["dy"], d["dres"], h, d["pre"], x=d["x"], post_weight=d["post"], gate=d["gate"], **k,
+                                     **kw)
+
+
+@pytest.mark.parametrize("T,H", SHAPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_forward_matches_oracle(ua, T, H, form):
+    d, r, k = _case(T, H, form)
+    h, y = _forward(ua, d, k)
+    (s64, y64), (s_size, y_size) = oracle.residual_norm_fp64(r["residual"], r["pre"], r["x"], r["post"], r["gate"], **k)
+    # sums of a row in a tree of at most 64 roundings, halved by the root, a dozen more for the products
+    if form[0]:
+        assert np.all(np.abs(gu.host_f64(h) - s64) <= (HALF + 4 * U) * np.abs(s64) + 64 * U * s_size)
+    else:
+        assert h is d["residual"]
+    if form[3]:
+        assert np.all(np.abs(gu.host_f64(y) - y64) <= (HALF + 4 * U) * np.abs(y64) + 128 * U * y_size)
+    else:
+        assert y is None
+
+
+@pytest.mark.parametrize("T,H", SHAPES)
+@pytest.mark.parametrize("form", FORMS)
+def test_backward_matches_oracle(ua, T, H, form):
+    d, r, k = _case(T, H, form, seed=1)
+    h = d["residual"]
+    got = dict(zip(("dresidual", "dx", "dpre", "dpost", "dgate"), _backward(ua, d, k, h)))
+    val, mag = oracle.residual_norm_backward_fp64(r["dy"], r["dres"], r["residual"], r["pre"], r["x"], r["post"], r["gate"],
+                                                  block=form[0], **k)
+    assert {n for n, t in got.items() if t is not None} == set(val)
+    for name, want in val.items():
+        t = got[name]
+        # a row's two norms in a row: the roots, means and products of each are under 256 roundings of their terms;
+        # sums over tokens: a group's rows one after another, then at most 256 groups
+        if t.dtype == __import__("torch").float32:
+            assert name in ("dpre", "dpost", "dgate") and tuple(t.shape) == (H,)
+            have, bound = t.cpu().numpy().astype(np.float64), (512 + T / 256 + 256) * U * mag[name]
+        else:
+            have, bound = gu.host_f64(t), (HALF + 4 * U) * np.abs(want) + 512 * U * mag[name]
+        assert have.shape == want.shape and np.all(np.abs(have - want) <= bound), name
+
+
+def test_gradient_is_the_difference_of_the_forward(ua):
+    """Central differences of the operator itself, along random directions: of y alone (the sum's own gradient is
+    dresidual_out by definition), at a residual large enough in bf16 that a step of a sixteenth is exact."""
+    T, H = 4, 64
+    d, r, k = _case(T, H, (True, True, "shared", True), seed=2)
+    (s, _), _ = oracle.residual_norm_fp64(r["residual"], r["pre"], r["x"], r["post"], r["gate"], **k)
+    h = gu.dev(oracle.to_bf16_bits(s))
+    d["dres"] = gu.dev(np.zeros((T, H), dtype=np.uint16))
+    grads = dict(zip(("residual", "x", "pre", "post", "gate"), _backward(ua, d, k, h)))
+    w = r["dy"]
+    for name, g in grads.items():
+        gv = g.double().cpu().numpy()
+        base = r[name]
+        step = 2.0 ** -5 * np.sign(np.random.default_rng(3).standard_normal(base.shape))
+        out = []
+        for sign in (1, -1):
+            moved = oracle.bf16_to_f64(oracle.to_bf16_bits(base + sign * step))
+            out.append((moved, dict(r, **{name: moved})))
+        loss = [float((w * oracle.residual_norm_fp64(v["residual"], v["pre"], v["x"], v["post"], v["gate"], **k)[0][1]).sum())
+                for _, v in out]
+        along = float((gv * (out[0][0] - out[1][0])).sum())
+        # second-order terms cancel; what stays is of third order in the step and the bf16 roundings of h and of the gradient
+        slack = 2.0 ** -7 * float((np.abs(gv) * np.abs(out[0][0] - out[1][0])).sum()) + 0.02 * abs(along) + 1e-2
+        assert abs(loss[0] - loss[1] - along) <= slack, name
+
+
+def test_rows_do_not_depend_on_the_batch(ua):
+    import torch
+    T, H = 333, 2048
+    d, _, k = _case(T, H, (True, True, "token", True), seed=3)
+    h, y = _forward(ua, d, k)
+    full = _backward(ua, d, k, h)
+    g = inputs.rng(301)
+    for n in (1, 2, 7, 40):
+        at = torch.from_numpy(g.permutation(T)[:n]).cuda()
+        part = {q: (t[at].contiguous() if t is not None and t.dim() == 2 else t) for q, t in d.items()}
+        hs, ys = _forward(ua, part, k)
+        assert torch.equal(hs, h[at]) and torch.equal(ys, y[at])
+        grads = _backward(ua, part, k, hs)
+        for i in (0, 1, 4):
+            assert torch.equal(grads[i], full[i][at])
+    again = _backward(ua, d, k, h)
+    assert all(torch.equal(a, b) for a, b in zip(again, full))
+
+
+@pytest.mark.parametrize("H", [64, 4096, 16384])
+def test_in_place_and_other_outputs(ua, H):
+    import torch
+    T = 300
+    d, _, k = _case(T, H, (True, True, "token", True), seed=4)
+    h, y = _forward(ua, d, k)
+    ref = _backward(ua, d, k, h)
+    e = {q: t.clone() for q, t in d.items()}
+    h2, y2 = ua.residual_norm(e["residual"], e["pre"], x=e["x"], post_weight=e["post"], gate=e["gate"], **k,
+                              residual_out=e["residual"], y=e["x"])
+    assert h2 is e["residual"] and y2 is e["x"] and torch.equal(h2, h) and torch.equal(y2, y)
+    e = {q: t.clone() for q, t in d.items()}
+    ws = torch.full((ua.residual_norm_backward_workspace_bytes(T, H),), 255, dtype=torch.uint8, device="cuda")
+    out = _backward(ua, e, k, h, dresidual=e["dres"], dx=e["dy"], workspace=ws)
+    assert out[0] is e["dres"] and out[1] is e["dy"] and all(torch.equal(a, b) for a, b in zip(out, ref))
+    r = d["residual"].clone()
+    _, want = ua.residual_norm(d["residual"], d["pre"])
+    assert torch.equal(ua.residual_norm(r, d["pre"], y=r)[1], want)
+
+
+def test_block_output_not_kept(ua):
+    """Without a norm or gate behind it the block's output is not read: its gradient comes without it."""
+    import torch
+    d, _, k = _case(50, 512, (True, False, "none", True), seed=5)
+    h, _ = _forward(ua, d, k)
+    want = _backward(ua, d, k, h)
+    got = ua.residual_norm_backward(d["dy"], d["dres"], h, d["pre"], has_block=True, **k)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    alone = ua.residual_norm_backward(d["dy"], d["dres"], h, d["pre"], **k)
+    assert alone[1] is None and torch.equal(alone[0], want[0])
+    # and without a gradient from above: the last norm of a model
+    top = ua.residual_norm_backward(d["dy"], None, h, d["pre"], has_block=True, **k)
+    zero = ua.residual_norm_backward(d["dy"], torch.zeros_like(h), h, d["pre"], has_block=True, **k)
+    assert all(torch.equal(a, b) for a, b in zip(top[:3], zero[:3]))
+
+
+def test_no_tokens(ua):
+    import torch
+    e = torch.empty((0, 256), dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(256, dtype=torch.bfloat16, device="cuda")
+    h, y = ua.residual_norm(e, w, x=e, post_weight=w, gate=w)
+    assert h.shape == y.shape == (0, 256)
+    dres, dx, dpre, dpost, dgate = ua.residual_norm_backward(e, e, e, w, x=e, post_weight=w, gate=w)
+    assert dres.shape == dx.shape == (0, 256) and not dpre.any() and not dpost.any() and not dgate.any()
+
+
+def test_zero_rows_large_rows_and_nan(ua):
+    import torch
+    H = 1024
+    w = torch.ones(H, dtype=torch.bfloat16, device="cuda")
+    r = torch.zeros((4, H), dtype=torch.bfloat16, device="cuda")
+    r[1] = 3.0e18    # the square of a bf16 value this large still fits fp32, with the sum of 1024 of them
+    r[2] = 1e-20     # squares below fp32's range: eps alone is left
+    r[3, 5] = float("nan")
+    _, y = ua.residual_norm(r, w, eps=1e-6)
+    assert not y[0].any() and torch.allclose(y[1].float(), torch.ones(H, device="cuda"), rtol=2 ** -8)
+    assert torch.allclose(y[2].float(), (r[2].float() * 1e3), rtol=2 ** -7) and torch.isnan(y[3]).all()
+    assert torch.isnan(ua.residual_norm(r[:1].contiguous(), w, eps=0.0)[1]).all()
+
+
+def test_captured_and_replayed(ua):
+    """Forward and gradients in one graph, replayed on new values, between eager calls of the same buffers' shapes."""
+    import torch
+    T, H = 130, 1024
+    form = (True, True, "shared", True)
+    d, _, k = _case(T, H, form, seed=6)
+    _backward(ua, d, k, _forward(ua, d, k)[0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        h, y = _forward(ua, d, k)
+        grads = _backward(ua, d, k, h)
+    for seed in (7, 8, 9):
+        e, _, _ = _case(T, H, form, seed=seed)
+        for q, t in d.items():
+            t.copy_(e[q])
+        g.replay()
+        torch.cuda.synchronize()
+        he, ye = _forward(ua, e, k)
+        want = _backward(ua, e, k, he)
+        assert torch.equal(h, he) and torch.equal(y, ye) and all(torch.equal(a, b) for a, b in zip(grads, want))
+
+
+def test_streams(ua):
+    """Two streams at once, outputs and workspaces allocated by the calls: each gets its own results."""
+    import torch
+    form = (True, True, "shared", True)
+    sets = [_case(400, 2048, form, seed=10 + i) for i in range(2)]
+    want = []
+    for d, _, k in sets:
+        h, y = _forward(ua, d, k)
+        want.append((h, y, _backward(ua, d, k, h)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for rep in range(5):
+        got = []
+        for (d, _, k), st in zip(sets, streams):
+            h, y = _forward(ua, d, k, stream=st if rep % 2 else st.cuda_stream)
+            got.append((h, y, _backward(ua, d, k, h, stream=st)))
+        torch.cuda.synchronize()
+        for (h, y, gr), (h2, y2, gr2) in zip(got, want):
+            assert torch.equal(h, h2) and torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(gr, gr2))
+
+
+def test_binding_refuses(ua):
+    import torch
+    t = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    bad = [lambda: ua.residual_norm(t), lambda: ua.residual_norm(t, w, gate=w), lambda: ua.residual_norm(t, w.float()),
+           lambda: ua.residual_norm(t, w, x=t[:2].contiguous()), lambda: ua.residual_norm(t, w, x=t, gate=t[:2].contiguous()),
+           lambda: ua.residual_norm(t[:, :32], w[:32]), lambda: ua.residual_norm(t.cpu(), w),
+           lambda: ua.residual_norm_backward(t, t, t), lambda: ua.residual_norm_backward(None, None, t, x=t),
+           lambda: ua.residual_norm_backward(t, t, t, w, post_weight=w),
+           lambda: ua.residual_norm_backward(t, t, t, w, dx=torch.empty_like(t))]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: ua.residual_norm(t, w, eps=-1.0), lambda: ua.residual_norm(t, w, x=t, scale=float("inf")),
+              lambda: ua.residual_norm(torch.zeros((1, 12), dtype=torch.bfloat16, device="cuda"), w[:12].contiguous()),
+              lambda: ua.residual_norm_backward(t, t, t, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(ua.UattnError):
+            f()
