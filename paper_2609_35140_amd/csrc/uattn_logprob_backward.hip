@@ -2,11 +2,15 @@
 //
 //   dlogits[v] = dlogp * inv_temperature * (1[v = target] - p_v),  p = softmax(logits * inv_temperature)
 //
-// One workgroup per row: the row's maximum and the sum of its exponentials (in an
-// order fixed by the vocabulary), then the gradient.  The target's own exponential
-// is left out of the sum and added last, so that 1 - p of the target is the
-// others' sum over the whole one: their difference from 1 would leave no digits
-// where the target is nearly certain.
+// One workgroup per row.  With k = inv_temperature * log2(e) every thread keeps a
+// running reference R = max x * k and the sum of exp2(fma(x, k, -R)); R's rounding
+// is common to all terms and leaves with the division.  The target's own
+// exponential is left out of the sum and added last, so that 1 - p of the target is
+// the others' sum over the whole one: their difference from 1 would leave no digits
+// where the target is nearly certain.  The order of the sum depends on the
+// vocabulary alone.
+#include <type_traits>
+
 #include "uattn_internal.h"
 #include "uattn_rows.h"
 
@@ -21,44 +25,146 @@ struct LogprobGradParams {
   int64_t stride, out_stride;
   int32_t vocab;
   float it, k;  // inverse temperature, and times log2(e)
-  int32_t first;
+  int32_t first;  // rows of the launches before this one
 };
 
-constexpr int kGradThreads = 1024;
+__device__ __forceinline__ float neg_infinity() { return -__builtin_inff(); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ float logit(const uint16_t* x, int v) { return bf16_lo(x[v]); }
+// A sum of exponentials relative to 2^ref.
+struct RefSum {
+  float ref, sum;
+};
+__device__ __forceinline__ float rebase(float from, float to) {
+  return from == neg_infinity() ? 0.f : exp2_of(from - to);
+}
+__device__ __forceinline__ RefSum combine(RefSum a, RefSum b) {
+  const float r = fmaxf(a.ref, b.ref);
+  return RefSum{r, a.sum * rebase(a.ref, r) + b.sum * rebase(b.ref, r)};
+}
+// What is subtracted from the exponents: a reference of -inf (nothing but masked entries) subtracts nothing.
+__device__ __forceinline__ float shift_of(float ref) { return ref == neg_infinity() ? 0.f : ref; }
 
-__global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradParams p) {
-  constexpr int kWaves = kGradThreads / 64;
-  __shared__ float slots[2][kWaves];
+// The row stays in registers between its sum and its gradient (kVecs 16-byte pieces to a thread, all
+// requested at once): it is read from memory once and written once.  Pieces past kThreads * kVecs are
+// read again.
+template <int kThreads, int kVecs>
+__global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParams p) {
+  constexpr int kWaves = kThreads / 64;
+  constexpr u32x4 kNegInf = {0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};
+  __shared__ RefSum parts[kWaves];
   const int64_t row = p.first + static_cast<int64_t>(blockIdx.x);
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint16_t* x = p.logits + row * p.stride;
   uint16_t* out = p.out + row * p.out_stride;
-  const int y = p.targets[row];
-  const float g = p.dlogp[row] * p.it;
-  float m = -__builtin_inff(), sum = 0.f;
-  const bool skip = p.dlogp[row] == 0.f, known = y >= 0 && y < p.vocab;
-  if (!skip) {
-    for (int v = tid; v < p.vocab; v += kGradThreads) m = __builtin_elementwise_maximum(m, logit(x, v));
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, d, 64));
-    if ((tid & 63) == 0) slots[0][tid >> 6] = m;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) m = __builtin_elementwise_maximum(m, slots[0][w]);
-    for (int v = tid; v < p.vocab; v += kGradThreads)
-      if (v != y) sum = sum + __builtin_amdgcn_exp2f((logit(x, v) - m) * p.k);
-    sum = block_sum<kWaves>(sum, slots[1]);
+  const int y = p.targets[row], pieces = p.vocab / 8, tail = 8 * pieces + tid;
+  const float dlogp = p.dlogp[row];
+  if (dlogp == 0.f) {
+    for (int v = tid; v < pieces; v += kThreads) store16(out, v, u32x4{0, 0, 0, 0});
+    if (tail < p.vocab) out[tail] = 0;
+    return;
   }
-  const float at = !skip && known ? __builtin_amdgcn_exp2f((logit(x, y) - m) * p.k) : 0.f;
-  const float inv = known ? 1.f / (sum + at) : __builtin_nanf("");
-  for (int v = tid; v < p.vocab; v += kGradThreads) {
-    float d = 0.f;
-    if (!skip) {
-      const float e = __builtin_amdgcn_exp2f((logit(x, v) - m) * p.k);
-      d = v == y ? g * (sum * inv) : -g * (e * inv);
+  const bool known = y >= 0 && y < p.vocab;
+  const int y_piece = known && y < 8 * pieces ? y >> 3 : -1;
+
+  u32x4 w[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int v0 = 64 * wave + i * kThreads;
+    w[i] = kNegInf;
+    if (v0 < pieces && v0 + lane < pieces) w[i] = load16(x, v0 + lane);
+  }
+  RefSum acc{neg_infinity(), 0.f};
+  // adds kN pieces, which begin at v0 + j * kThreads
+  auto add = [&](auto n_const, const u32x4* q, int v0) {
+    constexpr int kN = decltype(n_const)::value;
+    float m = neg_infinity();
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(bf16_lo(q[j][e]), bf16_hi(q[j][e])));
+    const float ref = fmaxf(acc.ref, m * p.k), shift = shift_of(ref);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      float t[8];
+      unpack8(q[j], t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = exp2_of(__builtin_fmaf(t[e], p.k, -shift));
+      const int at = y_piece - (v0 + j * kThreads);
+      if (at >= 0 && at < 64) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = lane == at && e == (y & 7) ? 0.f : t[e];
+      }
+      sum = sum + (((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
     }
-    out[v] = static_cast<uint16_t>(bf16_pair(d, d));
+    acc.sum = acc.sum * rebase(acc.ref, ref) + sum;
+    acc.ref = ref;
+  };
+  constexpr int kStep = 4;
+#pragma unroll
+  for (int i = 0; i < kVecs; i += kStep) {
+    const int v0 = 64 * wave + i * kThreads;
+    if (v0 >= pieces) break;
+    if constexpr (kVecs % kStep == 0) {
+      add(std::integral_constant<int, kStep>{}, w + i, v0);
+    } else {
+      if (i + kStep <= kVecs)
+        add(std::integral_constant<int, kStep>{}, w + i, v0);
+      else
+        add(std::integral_constant<int, kVecs % kStep>{}, w + i, v0);
+    }
+  }
+  for (int v0 = 64 * wave + kVecs * kThreads; v0 < pieces; v0 += kThreads) {
+    u32x4 q = kNegInf;
+    if (v0 + lane < pieces) q = load16(x, v0 + lane);
+    add(std::integral_constant<int, 1>{}, &q, v0);
+  }
+  if (tail < p.vocab) {
+    const float t = bf16_lo(x[tail]), ref = fmaxf(acc.ref, t * p.k);
+    acc.sum = acc.sum * rebase(acc.ref, ref) + (tail == y ? 0.f : exp2_of(__builtin_fmaf(t, p.k, -shift_of(ref))));
+    acc.ref = ref;
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1)
+    acc = combine(acc, RefSum{__shfl_xor(acc.ref, off, 64), __shfl_xor(acc.sum, off, 64)});
+  if constexpr (kWaves > 1) {
+    if (lane == 0) parts[wave] = acc;
+    __syncthreads();
+    acc = parts[0];
+#pragma unroll
+    for (int u = 1; u < kWaves; ++u) acc = combine(acc, parts[u]);
+  }
+  const float shift = shift_of(acc.ref), g = dlogp * p.it;
+  const float of_target = known ? exp2_of(__builtin_fmaf(bf16_lo(x[y]), p.k, -shift)) : 0.f;
+  const float inv = known ? 1.f / (acc.sum + of_target) : __builtin_nanf("");
+  const float scale = -g * inv, at_target = g * (acc.sum * inv);
+  auto put = [&](const u32x4& q, int v0) {
+    float t[8];
+    unpack8(q, t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = scale * exp2_of(__builtin_fmaf(t[e], p.k, -shift));
+    const int at = y_piece - v0;
+    if (at >= 0 && at < 64) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = lane == at && e == (y & 7) ? at_target : t[e];
+    }
+    if (v0 + lane < pieces) store16(out, v0 + lane, pack8(t));
+  };
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int v0 = 64 * wave + i * kThreads;
+    if (v0 >= pieces) break;
+    put(w[i], v0);
+  }
+  for (int v0 = 64 * wave + kVecs * kThreads; v0 < pieces; v0 += kThreads) {
+    u32x4 q = kNegInf;
+    if (v0 + lane < pieces) q = load16(x, v0 + lane);
+    put(q, v0);
+  }
+  if (tail < p.vocab) {
+    const float d = tail == y ? at_target : scale * exp2_of(__builtin_fmaf(bf16_lo(x[tail]), p.k, -shift));
+    out[tail] = static_cast<uint16_t>(bf16_pair(d, d));
   }
 }
 
@@ -75,10 +181,20 @@ hipError_t launch_logprob_backward(const LogprobBackwardLaunch& a, hipStream_t s
   p.vocab = a.vocab;
   p.it = a.inv_temperature;
   p.k = static_cast<float>(static_cast<double>(a.inv_temperature) * 1.4426950408889634);
-  return launch_parts(a.num_rows, kGradThreads, [&](int first, unsigned n) {
-    p.first = first;
-    hipLaunchKernelGGL(logprob_grad_kernel, dim3(n), dim3(kGradThreads), 0, stream, p);
-  });
+  auto launch = [&](auto threads_const, auto vecs_const) {
+    constexpr int kThreads = decltype(threads_const)::value, kVecs = decltype(vecs_const)::value;
+    return launch_parts(a.num_rows, kThreads, [&](int first, unsigned n) {
+      p.first = first;
+      hipLaunchKernelGGL((logprob_grad_kernel<kThreads, kVecs>), dim3(n), dim3(kThreads), 0, stream, p);
+    });
+  };
+  using std::integral_constant;
+  if (a.vocab <= 2048) return launch(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if (a.vocab <= 8192) return launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
+  if (a.vocab <= 32768) return launch(integral_constant<int, 256>{}, integral_constant<int, 16>{});
+  if (a.vocab <= 65536) return launch(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+  if (a.vocab <= 131072) return launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+  return launch(integral_constant<int, 1024>{}, integral_constant<int, 19>{});
 }
 
 }  // namespace uattn
