@@ -98,9 +98,18 @@ __global__ __launch_bounds__(kThreads) void residual_norm_kernel(NormParams p) {
 //   a = dy w_pre,  ds = dh' + r(h') (a - n mean(a n)),  dw_pre = sum_rows dy n
 //   b = scale ds gate,  dgate = scale ds u,  dw_post = sum_rows b m
 //   c = b w_post,  dx = r(x) (c - m mean(c m))           (dx = b without w_post)
-// A workgroup takes rows blockIdx, + gridDim, ... and keeps its share of the
-// column sums in registers; they go to the workspace, one set to a workgroup, and
-// a second kernel adds the sets in order.
+//
+// Bound by memory: five rows read and three written for a token at most.  A workgroup of sixteen
+// waves takes 16 / kRowWaves rows at a time (a wave handles 512 columns of a row, or twice 512), one
+// workgroup to a CU, and asks for its next rows before it works on these.  mean(a n) is
+// r(h') mean(a h'), so the sums of squares and this one meet in one exchange between the waves and
+// mean(c m) in a second.  The column sums stay in registers over all rows of the workgroup; the
+// workgroup's row groups add theirs through LDS, one set of sums to a workgroup goes to the
+// workspace, and a second kernel adds the sets.  Which rows share a set depends on the numbers of
+// tokens and columns alone.
+constexpr int kGradWaves = 16, kGradThreads = 64 * kGradWaves;
+constexpr int kMaxSets = 256;
+
 struct NormGradParams {
   const void *dy, *dresidual_out, *h, *pre, *x, *post, *gate;
   void *dresidual, *dx, *dgate_rows;
@@ -111,125 +120,197 @@ struct NormGradParams {
   int32_t pre_at, post_at, gate_at;  // which of the sums each is, or -1
 };
 
-template <int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads) void residual_norm_grad_kernel(NormGradParams p) {
-  constexpr int kWaves = kThreads / 64;
-  __shared__ float slots[4][kWaves];
-  const int tid = threadIdx.x, pieces = p.hidden / 8;
+// A token's pieces of one thread.
+template <int kVecs>
+struct GradRow {
+  u32x4 dy[kVecs], dr[kVecs], h[kVecs], x[kVecs], gate[kVecs];
+};
+
+template <int kRowWaves, int kVecs>
+__global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGradParams p) {
+  constexpr int kGroups = kGradWaves / kRowWaves;
+  __shared__ float4 squares[2][kGradWaves];
+  __shared__ float dots[2][kGradWaves];
+  __shared__ float columns[kGradThreads * 8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = wave / kRowWaves, in_row = (wave % kRowWaves) * 64 + lane;  // piece i: in_row + i * 64 * kRowWaves
+  const int pieces = p.hidden / 8;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+  const u32x4 zero = {0, 0, 0, 0};
+  auto piece = [&](int i) { return in_row + i * 64 * kRowWaves; };
+
+  u32x4 w_pre[kVecs], w_post[kVecs], w_gate[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int v = piece(i);
+    w_pre[i] = p.pre != nullptr && v < pieces ? load16(p.pre, v) : zero;
+    w_post[i] = p.post != nullptr && v < pieces ? load16(p.post, v) : zero;
+    w_gate[i] = p.gate != nullptr && p.gate_stride == 0 && v < pieces ? load16(p.gate, v) : zero;
+  }
   float dpre[kVecs][8] = {}, dpost[kVecs][8] = {}, dgate[kVecs][8] = {};
-  for (int64_t row = blockIdx.x; row < p.num_tokens; row += gridDim.x) {
-    const int64_t base = row * pieces;
-    const u32x4 zero = {0, 0, 0, 0};
+
+  // rows behind the last one read as zeros, which add nothing
+  auto load = [&](GradRow<kVecs>& d, int64_t row) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int v = piece(i);
+      const bool here = row < p.num_tokens && v < pieces;
+      const int64_t at = row * pieces + v;
+      d.dy[i] = d.dr[i] = d.h[i] = d.x[i] = zero;
+      d.gate[i] = w_gate[i];
+      if (!here) continue;
+      if (p.dresidual_out != nullptr) d.dr[i] = load16(p.dresidual_out, at);
+      if (p.dy != nullptr) {
+        d.h[i] = load16(p.h, at);
+        d.dy[i] = load16(p.dy, at);
+      }
+      if (p.x != nullptr) d.x[i] = load16(p.x, at);
+      if (p.gate_stride != 0 && p.gate != nullptr) d.gate[i] = load16(p.gate, at);
+    }
+  };
+
+  GradRow<kVecs> next;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  load(next, row);
+  int side = 0;
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups; row0 < p.num_tokens; row0 += step, row += step, side ^= 1) {
+    const GradRow<kVecs> d = next;
+    load(next, row + step);
+    const bool here = row < p.num_tokens;
+    float r = 0.f, dot = 0.f, rx = 1.f;
+    if (p.dy != nullptr || p.post != nullptr) {
+      float hh = 0.f, ah = 0.f, xx = 0.f;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        float h[8], a[8], w[8], x[8];
+        unpack8(d.h[i], h);
+        unpack8(d.dy[i], a);
+        unpack8(w_pre[i], w);
+        unpack8(d.x[i], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float t = h[e] * p.inv_hidden;
+          hh = __builtin_fmaf(t, h[e], hh);
+          ah = __builtin_fmaf(a[e] * w[e], t, ah);
+          xx = __builtin_fmaf(x[e] * p.inv_hidden, x[e], xx);
+        }
+      }
+      hh = wave_sum(hh);
+      ah = wave_sum(ah);
+      xx = wave_sum(xx);
+      if constexpr (kRowWaves > 1) {
+        if (lane == 0) squares[side][wave] = make_float4(hh, ah, xx, 0.f);
+        __syncthreads();
+        float4 t = squares[side][group * kRowWaves];
+#pragma unroll
+        for (int u = 1; u < kRowWaves; ++u) {
+          const float4 o = squares[side][group * kRowWaves + u];
+          t.x = t.x + o.x;
+          t.y = t.y + o.y;
+          t.z = t.z + o.z;
+        }
+        hh = t.x, ah = t.y, xx = t.z;
+      }
+      r = inverse_rms(hh, p.eps);
+      dot = r * ah;
+      if (p.post != nullptr) rx = inverse_rms(xx, p.eps);
+    }
     float ds[kVecs][8];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kThreads;
-      unpack8(p.dresidual_out != nullptr && v < pieces ? load16(p.dresidual_out, base + v) : zero, ds[i]);
-    }
-    if (p.dy != nullptr) {
-      float n[kVecs][8], a[kVecs][8], sq = 0.f;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const int v = tid + i * kThreads;
-        unpack8(v < pieces ? load16(p.h, base + v) : zero, n[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(n[i][e] * p.inv_hidden, n[i][e], sq);
-      }
-      const float r = inverse_rms(block_sum<kWaves>(sq, slots[0]), p.eps);
-      float dot = 0.f;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const int v = tid + i * kThreads;
-        float w[8];
-        unpack8(v < pieces ? load16(p.dy, base + v) : zero, a[i]);
-        unpack8(v < pieces ? load16(p.pre, v) : zero, w);
+      unpack8(d.dr[i], ds[i]);
+      if (p.dy != nullptr && here) {
+        float h[8], dy[8], w[8];
+        unpack8(d.h[i], h);
+        unpack8(d.dy[i], dy);
+        unpack8(w_pre[i], w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          n[i][e] = n[i][e] * r;
-          dpre[i][e] = dpre[i][e] + a[i][e] * n[i][e];
-          a[i][e] = a[i][e] * w[e];
-          dot = dot + a[i][e] * n[i][e];
+          const float n = h[e] * r;
+          dpre[i][e] = __builtin_fmaf(dy[e], n, dpre[i][e]);
+          ds[i][e] = __builtin_fmaf(r, __builtin_fmaf(-n, dot, dy[e] * w[e]), ds[i][e]);
         }
       }
-      dot = block_sum<kWaves>(dot, slots[1]) * p.inv_hidden;
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ds[i][e] = ds[i][e] + r * (a[i][e] - n[i][e] * dot);
+      if (here && piece(i) < pieces) store16(p.dresidual, row * pieces + piece(i), pack8(ds[i]));
     }
+    if (p.dx == nullptr) continue;
+    float m[kVecs][8], cm = 0.f;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kThreads;
-      if (v < pieces) store16(p.dresidual, base + v, pack8(ds[i]));
-    }
-    if (p.dx == nullptr) {
-      __syncthreads();
-      continue;
-    }
-    float m[kVecs][8], sq = 0.f, r = 1.f;
-    if (p.x != nullptr) {
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const int v = tid + i * kThreads;
-        unpack8(v < pieces ? load16(p.x, base + v) : zero, m[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(m[i][e] * p.inv_hidden, m[i][e], sq);
-      }
-      if (p.post != nullptr) r = inverse_rms(block_sum<kWaves>(sq, slots[2]), p.eps);
-    }
-    float dot = 0.f;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kThreads;
       float w[8], g[8];
-      unpack8(p.post != nullptr && v < pieces ? load16(p.post, v) : zero, w);
-      unpack8(p.gate != nullptr && v < pieces ? load16(p.gate, row * (p.gate_stride / 8) + v) : zero, g);
+      unpack8(d.x[i], m[i]);
+      unpack8(w_post[i], w);
+      unpack8(d.gate[i], g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        ds[i][e] = p.scale * ds[i][e];
-        if (p.post != nullptr) m[i][e] = m[i][e] * r;
-        if (p.gate != nullptr) {
-          const float u = p.post != nullptr ? m[i][e] * w[e] : m[i][e];
-          const float d = ds[i][e] * u;
-          dgate[i][e] = dgate[i][e] + d;
+      for (int e = 0; e < 8; ++e) ds[i][e] = p.scale * ds[i][e];
+      if (!here) continue;
+      if (p.post != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[i][e] = m[i][e] * rx;
+      }
+      if (p.gate != nullptr) {
+        float t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          t[e] = ds[i][e] * (p.post != nullptr ? m[i][e] * w[e] : m[i][e]);
+          dgate[i][e] = dgate[i][e] + t[e];
           ds[i][e] = ds[i][e] * g[e];
-          g[e] = d;
         }
-        if (p.post != nullptr) {
-          dpost[i][e] = dpost[i][e] + ds[i][e] * m[i][e];
+        if (p.dgate_rows != nullptr && piece(i) < pieces) store16(p.dgate_rows, row * pieces + piece(i), pack8(t));
+      }
+      if (p.post != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          dpost[i][e] = __builtin_fmaf(ds[i][e], m[i][e], dpost[i][e]);
           ds[i][e] = ds[i][e] * w[e];
-          dot = dot + ds[i][e] * m[i][e];
+          cm = __builtin_fmaf(ds[i][e] * p.inv_hidden, m[i][e], cm);
         }
       }
-      if (p.dgate_rows != nullptr && v < pieces) store16(p.dgate_rows, base + v, pack8(g));
     }
     if (p.post != nullptr) {
-      dot = block_sum<kWaves>(dot, slots[3]) * p.inv_hidden;
+      cm = wave_sum(cm);
+      if constexpr (kRowWaves > 1) {
+        if (lane == 0) dots[side][wave] = cm;
+        __syncthreads();
+        cm = dots[side][group * kRowWaves];
+#pragma unroll
+        for (int u = 1; u < kRowWaves; ++u) cm = cm + dots[side][group * kRowWaves + u];
+      }
 #pragma unroll
       for (int i = 0; i < kVecs; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ds[i][e] = r * (ds[i][e] - m[i][e] * dot);
+        for (int e = 0; e < 8; ++e) ds[i][e] = rx * __builtin_fmaf(-m[i][e], cm, ds[i][e]);
     }
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kThreads;
-      if (v < pieces) store16(p.dx, base + v, pack8(ds[i]));
-    }
-    __syncthreads();
+    for (int i = 0; i < kVecs; ++i)
+      if (here && piece(i) < pieces) store16(p.dx, row * pieces + piece(i), pack8(ds[i]));
   }
+  // the row groups' column sums, in the groups' order, by the first of them
+  auto put = [&](int at, const float(&d)[8], int v) {
+    if (at < 0) return;
+    float s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = d[e];
+    if constexpr (kGroups > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) columns[e * kGradThreads + tid] = d[e];
+      __syncthreads();
+      if (group != 0) return;
+      for (int u = 1; u < kGroups; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = s[e] + columns[e * kGradThreads + u * 64 * kRowWaves + tid];
+    }
+    if (v >= pieces) return;
+    float4* to = reinterpret_cast<float4*>(p.parts + (static_cast<int64_t>(at) * gridDim.x + blockIdx.x) * p.hidden) + 2 * v;
+    to[0] = make_float4(s[0], s[1], s[2], s[3]);
+    to[1] = make_float4(s[4], s[5], s[6], s[7]);
+  };
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
-    const int v = tid + i * kThreads;
-    if (v >= pieces) break;
-    auto put = [&](int at, const float(&d)[8]) {
-      if (at < 0) return;
-      float4* to = reinterpret_cast<float4*>(p.parts + (static_cast<int64_t>(at) * gridDim.x + blockIdx.x) * p.hidden) + 2 * v;
-      to[0] = make_float4(d[0], d[1], d[2], d[3]);
-      to[1] = make_float4(d[4], d[5], d[6], d[7]);
-    };
-    put(p.pre_at, dpre[i]);
-    put(p.post_at, dpost[i]);
-    put(p.gate_at, dgate[i]);
+    put(p.pre_at, dpre[i], piece(i));
+    put(p.post_at, dpost[i], piece(i));
+    put(p.gate_at, dgate[i], piece(i));
   }
 }
 
@@ -239,18 +320,44 @@ struct FoldParams {
   int32_t sets, hidden;
 };
 
-__global__ __launch_bounds__(64) void norm_fold_kernel(FoldParams p) {
-  const int col = blockIdx.x * 64 + threadIdx.x;
-  if (col >= p.hidden) return;
-  const float* in = p.parts + static_cast<int64_t>(blockIdx.y) * p.sets * p.hidden + col;
-  float s = 0.f;
-  for (int i = 0; i < p.sets; ++i) s = s + in[static_cast<int64_t>(i) * p.hidden];
-  p.out[blockIdx.y][col] = s;
+// Adds the sets: 64 columns to a workgroup, four to a thread, the sets s, s + 64, ... to the threads
+// of slot s, then the slots pairwise.
+constexpr int kFoldSlots = 64;
+__global__ __launch_bounds__(16 * kFoldSlots) void norm_fold_kernel(FoldParams p) {
+  __shared__ float4 slots[kFoldSlots][16];
+  const int quad = threadIdx.x & 15, slot = threadIdx.x >> 4, col = blockIdx.x * 64 + 4 * quad;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [](float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); };
+  if (col < p.hidden) {
+    const float* in = p.parts + static_cast<int64_t>(blockIdx.y) * p.sets * p.hidden + col;
+    float4 q[kMaxSets / kFoldSlots];
+#pragma unroll
+    for (int i = 0; i < kMaxSets / kFoldSlots; ++i) {
+      const int set = slot + i * kFoldSlots;
+      q[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (set < p.sets) q[i] = *reinterpret_cast<const float4*>(in + static_cast<int64_t>(set) * p.hidden);
+    }
+#pragma unroll
+    for (int i = 0; i < kMaxSets / kFoldSlots; ++i) s = add(s, q[i]);
+  }
+  for (int half = kFoldSlots / 2; half >= 1; half /= 2) {
+    slots[slot][quad] = s;
+    __syncthreads();
+    if (slot < half) s = add(s, slots[slot + half][quad]);
+    __syncthreads();
+  }
+  if (slot == 0 && col < p.hidden) *reinterpret_cast<float4*>(p.out[blockIdx.y] + col) = s;
 }
 
-constexpr int kMaxSets = 256;
+// Rows a workgroup takes at a time.
+int grad_groups(int64_t hidden_dim) {
+  return hidden_dim <= 512 ? 16 : hidden_dim <= 1024 ? 8 : hidden_dim <= 2048 ? 4 : hidden_dim <= 4096 ? 2 : 1;
+}
 
-int norm_sets(int64_t num_tokens) { return static_cast<int>(num_tokens < kMaxSets ? num_tokens : kMaxSets); }
+int norm_sets(int64_t num_tokens, int64_t hidden_dim) {
+  const int64_t sets = (num_tokens + grad_groups(hidden_dim) - 1) / grad_groups(hidden_dim);
+  return static_cast<int>(sets < kMaxSets ? sets : kMaxSets);
+}
 
 }  // namespace
 
@@ -271,7 +378,7 @@ hipError_t launch_residual_norm(const ResidualNormLaunch& a, hipStream_t stream)
 }
 
 size_t residual_norm_backward_ws_bytes(int64_t num_tokens, int64_t hidden_dim) {
-  return static_cast<size_t>(3) * norm_sets(num_tokens) * hidden_dim * sizeof(float);
+  return static_cast<size_t>(3) * norm_sets(num_tokens, hidden_dim) * hidden_dim * sizeof(float);
 }
 
 hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hipStream_t stream) {
@@ -295,7 +402,7 @@ hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hi
   p.hidden = a.hidden_dim;
   FoldParams f{};
   f.parts = p.parts;
-  f.sets = norm_sets(a.num_tokens);
+  f.sets = norm_sets(a.num_tokens, a.hidden_dim);
   f.hidden = a.hidden_dim;
   int sums = 0;
   auto sum_of = [&](float* out) {
@@ -307,24 +414,28 @@ hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hi
   p.post_at = sum_of(a.dpost_weight);
   p.gate_at = sum_of(a.gate_stride == 0 ? static_cast<float*>(a.dgate) : nullptr);
   if (f.sets > 0) {
-    auto launch = [&](auto threads, auto vecs) {
-      hipLaunchKernelGGL((residual_norm_grad_kernel<decltype(threads)::value, decltype(vecs)::value>), dim3(f.sets),
-                         dim3(decltype(threads)::value), 0, stream, p);
+    auto launch = [&](auto row_waves, auto vecs) {
+      hipLaunchKernelGGL((residual_norm_grad_kernel<decltype(row_waves)::value, decltype(vecs)::value>), dim3(f.sets),
+                         dim3(kGradThreads), 0, stream, p);
     };
     using std::integral_constant;
-    if (a.hidden_dim <= 2048)
-      launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-    else if (a.hidden_dim <= 4096)
-      launch(integral_constant<int, 512>{}, integral_constant<int, 1>{});
-    else if (a.hidden_dim <= 8192)
-      launch(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
-    else
-      launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    const integral_constant<int, 1> one;
+    switch (grad_groups(a.hidden_dim)) {
+      case 16: launch(one, one); break;
+      case 8: launch(integral_constant<int, 2>{}, one); break;
+      case 4: launch(integral_constant<int, 4>{}, one); break;
+      case 2: launch(integral_constant<int, 8>{}, one); break;
+      default:
+        if (a.hidden_dim <= 8192)
+          launch(integral_constant<int, 16>{}, one);
+        else
+          launch(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (sums > 0) {
-    hipLaunchKernelGGL(norm_fold_kernel, dim3((a.hidden_dim + 63) / 64, sums), dim3(64), 0, stream, f);
+    hipLaunchKernelGGL(norm_fold_kernel, dim3((a.hidden_dim + 63) / 64, sums), dim3(16 * kFoldSlots), 0, stream, f);
     return hipGetLastError();
   }
   return hipSuccess;
