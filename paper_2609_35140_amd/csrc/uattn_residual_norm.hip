@@ -22,57 +22,70 @@ struct NormParams {
   void *residual_out, *y;
   int64_t gate_stride;
   float scale, eps, inv_hidden;
-  int32_t hidden;
+  int32_t num_tokens, hidden;
   int32_t first;  // rows of the launches before this one
 };
 
 __device__ __forceinline__ float inverse_rms(float mean, float eps) { return 1.0f / __builtin_sqrtf(mean + eps); }
 
-template <int kThreads, int kVecs>
-__global__ __launch_bounds__(kThreads) void residual_norm_kernel(NormParams p) {
-  constexpr int kWaves = kThreads / 64;
+// A row is taken by kRowWaves waves, kVecs pieces to a thread; a workgroup has four waves, or a row's
+// where that is more.  Bound by memory.
+template <int kRowWaves>
+constexpr int kNormWaves = kRowWaves > 4 ? kRowWaves : 4;
+
+template <int kRowWaves, int kVecs>
+__global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kernel(NormParams p) {
+  constexpr int kWaves = kNormWaves<kRowWaves>, kRows = kWaves / kRowWaves;
   __shared__ float slots[2][kWaves];
-  const int tid = threadIdx.x, pieces = p.hidden / 8;
-  const int64_t row = p.first + static_cast<int64_t>(blockIdx.x), base = row * pieces;
-  float s[kVecs][8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = wave / kRowWaves, wave0 = group * kRowWaves, in_row = (wave - wave0) * 64 + lane;
+  const int pieces = p.hidden / 8;
+  const int64_t row = p.first + static_cast<int64_t>(blockIdx.x) * kRows + group, base = row * pieces;
+  const bool here = row < p.num_tokens;
+  auto piece = [&](int i) { return in_row + i * 64 * kRowWaves; };
+  const u32x4 zero = {0, 0, 0, 0};
+  u32x4 hw[kVecs], xw[kVecs];
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
-    const int v = tid + i * kThreads;
-    u32x4 w = {0, 0, 0, 0};
-    if (v < pieces) w = load16(p.residual, base + v);
-    unpack8(w, s[i]);
+    hw[i] = xw[i] = zero;
+    if (!here || piece(i) >= pieces) continue;
+    hw[i] = load16(p.residual, base + piece(i));
+    if (p.x != nullptr) xw[i] = load16(p.x, base + piece(i));
   }
+  float s[kVecs][8];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) unpack8(hw[i], s[i]);
   if (p.x != nullptr) {
-    float u[kVecs][8], sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kThreads;
-      u32x4 w = {0, 0, 0, 0};
-      if (v < pieces) w = load16(p.x, base + v);
-      unpack8(w, u[i]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(u[i][e] * p.inv_hidden, u[i][e], sum);
-    }
     float r = 1.f;
-    if (p.post != nullptr) r = inverse_rms(block_sum<kWaves>(sum, slots[0]), p.eps);
+    if (p.post != nullptr) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        float u[8];
+        unpack8(xw[i], u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(u[e] * p.inv_hidden, u[e], sum);
+      }
+      r = inverse_rms(waves_sum<kRowWaves>(sum, slots[0], wave, wave0), p.eps);
+    }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kThreads;
-      if (v >= pieces) break;
-      float g[8];
+      if (!here || piece(i) >= pieces) break;
+      float u[8], g[8];
+      unpack8(xw[i], u);
       if (p.post != nullptr) {
-        unpack8(load16(p.post, v), g);
+        unpack8(load16(p.post, piece(i)), g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[i][e] = u[i][e] * r * g[e];
+        for (int e = 0; e < 8; ++e) u[e] = u[e] * r * g[e];
       }
       if (p.gate != nullptr) {
-        unpack8(load16(p.gate, row * (p.gate_stride / 8) + v), g);
+        unpack8(load16(p.gate, row * (p.gate_stride / 8) + piece(i)), g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[i][e] = u[i][e] * g[e];
+        for (int e = 0; e < 8; ++e) u[e] = u[e] * g[e];
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[i][e] = s[i][e] + p.scale * u[i][e];
-      store16(p.residual_out, base + v, pack8(s[i]));
+      for (int e = 0; e < 8; ++e) s[i][e] = __builtin_fmaf(p.scale, u[e], s[i][e]);
+      store16(p.residual_out, base + piece(i), pack8(s[i]));
     }
   }
   if (p.y == nullptr) return;
@@ -81,16 +94,15 @@ __global__ __launch_bounds__(kThreads) void residual_norm_kernel(NormParams p) {
   for (int i = 0; i < kVecs; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(s[i][e] * p.inv_hidden, s[i][e], sum);
-  const float r = inverse_rms(block_sum<kWaves>(sum, slots[1]), p.eps);
+  const float r = inverse_rms(waves_sum<kRowWaves>(sum, slots[1], wave, wave0), p.eps);
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
-    const int v = tid + i * kThreads;
-    if (v >= pieces) break;
+    if (!here || piece(i) >= pieces) break;
     float g[8];
-    unpack8(load16(p.pre, v), g);
+    unpack8(load16(p.pre, piece(i)), g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) g[e] = s[i][e] * r * g[e];
-    store16(p.y, base + v, pack8(g));
+    store16(p.y, base + piece(i), pack8(g));
   }
 }
 
@@ -126,7 +138,7 @@ struct GradRow {
   u32x4 dy[kVecs], dr[kVecs], h[kVecs], x[kVecs], gate[kVecs];
 };
 
-template <int kRowWaves, int kVecs>
+template <int kRowWaves, int kVecs, bool kAhead>
 __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGradParams p) {
   constexpr int kGroups = kGradWaves / kRowWaves;
   __shared__ float4 squares[2][kGradWaves];
@@ -139,16 +151,23 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
   const u32x4 zero = {0, 0, 0, 0};
   auto piece = [&](int i) { return in_row + i * 64 * kRowWaves; };
 
+  // the weights stay in registers where the next rows do, and come from the cache where they are used otherwise
   u32x4 w_pre[kVecs], w_post[kVecs], w_gate[kVecs];
+  auto weight = [&](const void* w, int i) { return w != nullptr && piece(i) < pieces ? load16(w, piece(i)) : zero; };
+  const void* shared_gate = p.gate_stride == 0 ? p.gate : nullptr;
+  if constexpr (kAhead) {
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    const int v = piece(i);
-    w_pre[i] = p.pre != nullptr && v < pieces ? load16(p.pre, v) : zero;
-    w_post[i] = p.post != nullptr && v < pieces ? load16(p.post, v) : zero;
-    w_gate[i] = p.gate != nullptr && p.gate_stride == 0 && v < pieces ? load16(p.gate, v) : zero;
+    for (int i = 0; i < kVecs; ++i) {
+      w_pre[i] = weight(p.pre, i);
+      w_post[i] = weight(p.post, i);
+      w_gate[i] = weight(shared_gate, i);
+    }
   }
+  auto pre_of = [&](int i) { return kAhead ? w_pre[i] : weight(p.pre, i); };
+  auto post_of = [&](int i) { return kAhead ? w_post[i] : weight(p.post, i); };
   float dpre[kVecs][8] = {}, dpost[kVecs][8] = {}, dgate[kVecs][8] = {};
 
+  const bool reads_x = p.post != nullptr || p.gate != nullptr;
   // rows behind the last one read as zeros, which add nothing
   auto load = [&](GradRow<kVecs>& d, int64_t row) {
 #pragma unroll
@@ -157,25 +176,26 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
       const bool here = row < p.num_tokens && v < pieces;
       const int64_t at = row * pieces + v;
       d.dy[i] = d.dr[i] = d.h[i] = d.x[i] = zero;
-      d.gate[i] = w_gate[i];
+      d.gate[i] = kAhead ? w_gate[i] : zero;
       if (!here) continue;
       if (p.dresidual_out != nullptr) d.dr[i] = load16(p.dresidual_out, at);
       if (p.dy != nullptr) {
         d.h[i] = load16(p.h, at);
         d.dy[i] = load16(p.dy, at);
       }
-      if (p.x != nullptr) d.x[i] = load16(p.x, at);
+      if (reads_x) d.x[i] = load16(p.x, at);
       if (p.gate_stride != 0 && p.gate != nullptr) d.gate[i] = load16(p.gate, at);
     }
   };
 
   GradRow<kVecs> next;
   int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + group;
-  load(next, row);
+  if constexpr (kAhead) load(next, row);
   int side = 0;
   for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups; row0 < p.num_tokens; row0 += step, row += step, side ^= 1) {
+    if constexpr (!kAhead) load(next, row);
     const GradRow<kVecs> d = next;
-    load(next, row + step);
+    if constexpr (kAhead) load(next, row + step);
     const bool here = row < p.num_tokens;
     float r = 0.f, dot = 0.f, rx = 1.f;
     if (p.dy != nullptr || p.post != nullptr) {
@@ -185,7 +205,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
         float h[8], a[8], w[8], x[8];
         unpack8(d.h[i], h);
         unpack8(d.dy[i], a);
-        unpack8(w_pre[i], w);
+        unpack8(pre_of(i), w);
         unpack8(d.x[i], x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -201,15 +221,10 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
       if constexpr (kRowWaves > 1) {
         if (lane == 0) squares[side][wave] = make_float4(hh, ah, xx, 0.f);
         __syncthreads();
-        float4 t = squares[side][group * kRowWaves];
-#pragma unroll
-        for (int u = 1; u < kRowWaves; ++u) {
-          const float4 o = squares[side][group * kRowWaves + u];
-          t.x = t.x + o.x;
-          t.y = t.y + o.y;
-          t.z = t.z + o.z;
-        }
-        hh = t.x, ah = t.y, xx = t.z;
+        const float4 t = squares[side][group * kRowWaves + (lane & (kRowWaves - 1))];
+        hh = period_sum<kRowWaves>(t.x);
+        ah = period_sum<kRowWaves>(t.y);
+        xx = period_sum<kRowWaves>(t.z);
       }
       r = inverse_rms(hh, p.eps);
       dot = r * ah;
@@ -223,7 +238,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
         float h[8], dy[8], w[8];
         unpack8(d.h[i], h);
         unpack8(d.dy[i], dy);
-        unpack8(w_pre[i], w);
+        unpack8(pre_of(i), w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float n = h[e] * r;
@@ -234,25 +249,25 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
       if (here && piece(i) < pieces) store16(p.dresidual, row * pieces + piece(i), pack8(ds[i]));
     }
     if (p.dx == nullptr) continue;
-    float m[kVecs][8], cm = 0.f;
+    float cm = 0.f;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      float w[8], g[8];
-      unpack8(d.x[i], m[i]);
-      unpack8(w_post[i], w);
-      unpack8(d.gate[i], g);
+      float m[8], w[8], g[8];
+      unpack8(d.x[i], m);
+      unpack8(post_of(i), w);
+      unpack8(kAhead || shared_gate == nullptr ? d.gate[i] : weight(shared_gate, i), g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) ds[i][e] = p.scale * ds[i][e];
       if (!here) continue;
       if (p.post != nullptr) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[i][e] = m[i][e] * rx;
+        for (int e = 0; e < 8; ++e) m[e] = m[e] * rx;
       }
       if (p.gate != nullptr) {
         float t[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          t[e] = ds[i][e] * (p.post != nullptr ? m[i][e] * w[e] : m[i][e]);
+          t[e] = ds[i][e] * (p.post != nullptr ? m[e] * w[e] : m[e]);
           dgate[i][e] = dgate[i][e] + t[e];
           ds[i][e] = ds[i][e] * g[e];
         }
@@ -261,25 +276,21 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
       if (p.post != nullptr) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          dpost[i][e] = __builtin_fmaf(ds[i][e], m[i][e], dpost[i][e]);
+          dpost[i][e] = __builtin_fmaf(ds[i][e], m[e], dpost[i][e]);
           ds[i][e] = ds[i][e] * w[e];
-          cm = __builtin_fmaf(ds[i][e] * p.inv_hidden, m[i][e], cm);
+          cm = __builtin_fmaf(ds[i][e] * p.inv_hidden, m[e], cm);
         }
       }
     }
     if (p.post != nullptr) {
-      cm = wave_sum(cm);
-      if constexpr (kRowWaves > 1) {
-        if (lane == 0) dots[side][wave] = cm;
-        __syncthreads();
-        cm = dots[side][group * kRowWaves];
+      cm = waves_sum<kRowWaves>(cm, dots[side], wave, group * kRowWaves);
 #pragma unroll
-        for (int u = 1; u < kRowWaves; ++u) cm = cm + dots[side][group * kRowWaves + u];
+      for (int i = 0; i < kVecs; ++i) {
+        float x[8];
+        unpack8(d.x[i], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ds[i][e] = rx * __builtin_fmaf(-(x[e] * rx), cm, ds[i][e]);
       }
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ds[i][e] = rx * __builtin_fmaf(-m[i][e], cm, ds[i][e]);
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
@@ -363,18 +374,26 @@ int norm_sets(int64_t num_tokens, int64_t hidden_dim) {
 
 hipError_t launch_residual_norm(const ResidualNormLaunch& a, hipStream_t stream) {
   NormParams p{a.x, a.post_weight, a.gate, a.residual, a.pre_weight, a.residual_out, a.y, a.gate_stride, a.scale, a.eps,
-               1.0f / a.hidden_dim, a.hidden_dim, 0};
-  auto launch = [&](auto vecs) {
-    return launch_parts(a.num_tokens, 256, [&](int first, unsigned n) {
-      p.first = first;
-      hipLaunchKernelGGL((residual_norm_kernel<256, decltype(vecs)::value>), dim3(n), dim3(256), 0, stream, p);
+               1.0f / a.hidden_dim, a.num_tokens, a.hidden_dim, 0};
+  auto launch = [&](auto row_waves, auto vecs) {
+    constexpr int kRowWaves = decltype(row_waves)::value, kVecs = decltype(vecs)::value;
+    constexpr int kWaves = kNormWaves<kRowWaves>, kRows = kWaves / kRowWaves;
+    return launch_parts((static_cast<int64_t>(a.num_tokens) + kRows - 1) / kRows, 64 * kWaves, [&](int first, unsigned n) {
+      p.first = first * kRows;
+      hipLaunchKernelGGL((residual_norm_kernel<kRowWaves, kVecs>), dim3(n), dim3(64 * kWaves), 0, stream, p);
     });
   };
   using std::integral_constant;
-  if (a.hidden_dim <= 2048) return launch(integral_constant<int, 1>{});
-  if (a.hidden_dim <= 4096) return launch(integral_constant<int, 2>{});
-  if (a.hidden_dim <= 8192) return launch(integral_constant<int, 4>{});
-  return launch(integral_constant<int, 8>{});
+  const integral_constant<int, 1> one;
+  const integral_constant<int, 2> two;
+  const integral_constant<int, 4> four;
+  const integral_constant<int, 8> eight;
+  if (a.hidden_dim <= 512) return launch(one, one);
+  if (a.hidden_dim <= 1024) return launch(one, two);
+  if (a.hidden_dim <= 2048) return launch(one, four);
+  if (a.hidden_dim <= 4096) return launch(four, two);
+  if (a.hidden_dim <= 8192) return launch(eight, two);
+  return launch(eight, four);
 }
 
 size_t residual_norm_backward_ws_bytes(int64_t num_tokens, int64_t hidden_dim) {
@@ -415,7 +434,7 @@ hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hi
   p.gate_at = sum_of(a.gate_stride == 0 ? static_cast<float*>(a.dgate) : nullptr);
   if (f.sets > 0) {
     auto launch = [&](auto row_waves, auto vecs) {
-      hipLaunchKernelGGL((residual_norm_grad_kernel<decltype(row_waves)::value, decltype(vecs)::value>), dim3(f.sets),
+      hipLaunchKernelGGL((residual_norm_grad_kernel<decltype(row_waves)::value, decltype(vecs)::value, decltype(vecs)::value == 1>), dim3(f.sets),
                          dim3(kGradThreads), 0, stream, p);
     };
     using std::integral_constant;

@@ -63,19 +63,28 @@ __device__ __forceinline__ float wave_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// The sum over a workgroup of kWaves waves, in every thread: wave sums through `slots`, added in
-// wave order.  Calls in a row take different slots (one barrier each), so that a wave that is ahead
-// does not overwrite what another still reads.
+// The sum over kWaves values (a power of two up to 16) that lanes l, l + kWaves, ... hold alike, in every lane.
 template <int kWaves>
-__device__ __forceinline__ float block_sum(float x, float* slots) {
+__device__ __forceinline__ float period_sum(float x) {
+  if constexpr (kWaves > 8) x = x + dpp_read<0x128>(x);  // row_ror:8
+  if constexpr (kWaves > 4) x = x + dpp_read<0x124>(x);  // row_ror:4
+  if constexpr (kWaves > 2) x = x + dpp_read<0x4E>(x);   // lane ^ 2
+  if constexpr (kWaves > 1) x = x + dpp_read<0xB1>(x);   // lane ^ 1
+  return x;
+}
+
+// The sum over kWaves waves whose first is `wave0`, in every thread of theirs: wave sums through
+// `slots` (one to a wave of the workgroup), every lane reading one of them.  All of the workgroup
+// passes the barrier.  Calls in a row take different slots, so that a wave that is ahead does not
+// overwrite what another still reads.
+template <int kWaves>
+__device__ __forceinline__ float waves_sum(float x, float* slots, int wave, int wave0) {
   x = wave_sum(x);
   if constexpr (kWaves == 1) return x;
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = x;
+  const int lane = threadIdx.x & 63;
+  if (lane == 0) slots[wave] = x;
   __syncthreads();
-  float s = slots[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) s = s + slots[w];
-  return s;
+  return period_sum<kWaves>(slots[wave0 + (lane & (kWaves - 1))]);
 }
 
 }  // namespace uattn
