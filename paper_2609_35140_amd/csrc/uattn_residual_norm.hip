@@ -111,9 +111,9 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
 //   b = scale ds gate,  dgate = scale ds u,  dw_post = sum_rows b m
 //   c = b w_post,  dx = r(x) (c - m mean(c m))           (dx = b without w_post)
 //
-// Bound by memory: five rows read and three written for a token at most.  A workgroup of sixteen
-// waves takes 16 / kRowWaves rows at a time (a wave handles 512 columns of a row, or twice 512), one
-// workgroup to a CU, and asks for its next rows before it works on these.  mean(a n) is
+// Bound by memory: five rows read and three written for a token at most.  A workgroup of up to sixteen
+// waves, one to a CU, takes as many rows at a time as have room (a wave handles 512 columns of a row,
+// or twice 512), and asks for its next rows before it works on these.  mean(a n) is
 // r(h') mean(a h'), so the sums of squares and this one meet in one exchange between the waves and
 // mean(c m) in a second.  The column sums stay in registers over all rows of the workgroup; the
 // workgroup's row groups add theirs through LDS, one set of sums to a workgroup goes to the
@@ -129,6 +129,7 @@ struct NormGradParams {
   int64_t gate_stride;
   float scale, eps, inv_hidden;
   int32_t num_tokens, hidden;
+  int32_t row_waves, groups;  // waves to a row, rows to a workgroup at a time
   int32_t pre_at, post_at, gate_at;  // which of the sums each is, or -1
 };
 
@@ -138,18 +139,20 @@ struct GradRow {
   u32x4 dy[kVecs], dr[kVecs], h[kVecs], x[kVecs], gate[kVecs];
 };
 
-template <int kRowWaves, int kVecs, bool kAhead>
+template <int kVecs, bool kAhead>
 __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGradParams p) {
-  constexpr int kGroups = kGradWaves / kRowWaves;
   __shared__ float4 squares[2][kGradWaves];
   __shared__ float dots[2][kGradWaves];
-  __shared__ float columns[kGradThreads * 8];
+  // the groups' meeting place; with two pieces to a thread (one group) the place of two of the three column sums, for
+  // which the registers have no room
+  __shared__ float4 columns[kGradThreads * (kVecs == 1 ? 2 : 4 * kVecs)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int group = wave / kRowWaves, in_row = (wave % kRowWaves) * 64 + lane;  // piece i: in_row + i * 64 * kRowWaves
+  const int row_waves = p.row_waves, groups = p.groups;
+  const int group = wave / row_waves, wave0 = group * row_waves, in_row = (wave - wave0) * 64 + lane;
   const int pieces = p.hidden / 8;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * groups;
   const u32x4 zero = {0, 0, 0, 0};
-  auto piece = [&](int i) { return in_row + i * 64 * kRowWaves; };
+  auto piece = [&](int i) { return in_row + i * 64 * row_waves; };
 
   // the weights stay in registers where the next rows do, and come from the cache where they are used otherwise
   u32x4 w_pre[kVecs], w_post[kVecs], w_gate[kVecs];
@@ -166,6 +169,23 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
   auto pre_of = [&](int i) { return kAhead ? w_pre[i] : weight(p.pre, i); };
   auto post_of = [&](int i) { return kAhead ? w_post[i] : weight(p.post, i); };
   float dpre[kVecs][8] = {}, dpost[kVecs][8] = {}, dgate[kVecs][8] = {};
+  // the two float4 of piece i of dpost (which = 0) and dgate (1)
+  auto held = [&](int which, int i, int half) -> float4& { return columns[((which * kVecs + i) * 2 + half) * kGradThreads + tid]; };
+  if constexpr (kVecs > 1) {
+#pragma unroll
+    for (int u = 0; u < 4 * kVecs; ++u) columns[u * kGradThreads + tid] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  auto add_held = [&](int which, int i, const float(&d)[8]) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      float4 t = held(which, i, half);
+      t.x = t.x + d[4 * half];
+      t.y = t.y + d[4 * half + 1];
+      t.z = t.z + d[4 * half + 2];
+      t.w = t.w + d[4 * half + 3];
+      held(which, i, half) = t;
+    }
+  };
 
   const bool reads_x = p.post != nullptr || p.gate != nullptr;
   // rows behind the last one read as zeros, which add nothing
@@ -174,25 +194,25 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
     for (int i = 0; i < kVecs; ++i) {
       const int v = piece(i);
       const bool here = row < p.num_tokens && v < pieces;
-      const int64_t at = row * pieces + v;
+      const int64_t at = row * pieces;
       d.dy[i] = d.dr[i] = d.h[i] = d.x[i] = zero;
       d.gate[i] = kAhead ? w_gate[i] : zero;
       if (!here) continue;
-      if (p.dresidual_out != nullptr) d.dr[i] = load16(p.dresidual_out, at);
+      if (p.dresidual_out != nullptr) d.dr[i] = load16(p.dresidual_out, at, v);
       if (p.dy != nullptr) {
-        d.h[i] = load16(p.h, at);
-        d.dy[i] = load16(p.dy, at);
+        d.h[i] = load16(p.h, at, v);
+        d.dy[i] = load16(p.dy, at, v);
       }
-      if (reads_x) d.x[i] = load16(p.x, at);
-      if (p.gate_stride != 0 && p.gate != nullptr) d.gate[i] = load16(p.gate, at);
+      if (reads_x) d.x[i] = load16(p.x, at, v);
+      if (p.gate_stride != 0 && p.gate != nullptr) d.gate[i] = load16(p.gate, at, v);
     }
   };
 
   GradRow<kVecs> next;
-  int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * groups + group;
   if constexpr (kAhead) load(next, row);
   int side = 0;
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kGroups; row0 < p.num_tokens; row0 += step, row += step, side ^= 1) {
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * groups; row0 < p.num_tokens; row0 += step, row += step, side ^= 1) {
     if constexpr (!kAhead) load(next, row);
     const GradRow<kVecs> d = next;
     if constexpr (kAhead) load(next, row + step);
@@ -218,13 +238,14 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
       hh = wave_sum(hh);
       ah = wave_sum(ah);
       xx = wave_sum(xx);
-      if constexpr (kRowWaves > 1) {
+      if (row_waves > 1) {
         if (lane == 0) squares[side][wave] = make_float4(hh, ah, xx, 0.f);
         __syncthreads();
-        const float4 t = squares[side][group * kRowWaves + (lane & (kRowWaves - 1))];
-        hh = period_sum<kRowWaves>(t.x);
-        ah = period_sum<kRowWaves>(t.y);
-        xx = period_sum<kRowWaves>(t.z);
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        if ((lane & 15) < row_waves) t = squares[side][wave0 + (lane & 15)];
+        hh = period_sum<16>(t.x);
+        ah = period_sum<16>(t.y);
+        xx = period_sum<16>(t.z);
       }
       r = inverse_rms(hh, p.eps);
       dot = r * ah;
@@ -246,7 +267,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
           ds[i][e] = __builtin_fmaf(r, __builtin_fmaf(-n, dot, dy[e] * w[e]), ds[i][e]);
         }
       }
-      if (here && piece(i) < pieces) store16(p.dresidual, row * pieces + piece(i), pack8(ds[i]));
+      if (here && piece(i) < pieces) store16(p.dresidual, row * pieces, piece(i), pack8(ds[i]));
     }
     if (p.dx == nullptr) continue;
     float cm = 0.f;
@@ -268,22 +289,35 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           t[e] = ds[i][e] * (p.post != nullptr ? m[e] * w[e] : m[e]);
-          dgate[i][e] = dgate[i][e] + t[e];
+          if constexpr (kVecs == 1) dgate[i][e] = dgate[i][e] + t[e];
           ds[i][e] = ds[i][e] * g[e];
         }
-        if (p.dgate_rows != nullptr && piece(i) < pieces) store16(p.dgate_rows, row * pieces + piece(i), pack8(t));
+        if constexpr (kVecs > 1)
+          if (p.gate_at >= 0) add_held(1, i, t);
+        if (p.dgate_rows != nullptr && piece(i) < pieces) store16(p.dgate_rows, row * pieces, piece(i), pack8(t));
       }
       if (p.post != nullptr) {
+        if constexpr (kVecs > 1) {
+          float t[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[e] = ds[i][e] * m[e];
+          add_held(0, i, t);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          dpost[i][e] = __builtin_fmaf(ds[i][e], m[e], dpost[i][e]);
+          if constexpr (kVecs == 1) dpost[i][e] = __builtin_fmaf(ds[i][e], m[e], dpost[i][e]);
           ds[i][e] = ds[i][e] * w[e];
           cm = __builtin_fmaf(ds[i][e] * p.inv_hidden, m[e], cm);
         }
       }
     }
     if (p.post != nullptr) {
-      cm = waves_sum<kRowWaves>(cm, dots[side], wave, group * kRowWaves);
+      cm = wave_sum(cm);
+      if (row_waves > 1) {
+        if (lane == 0) dots[side][wave] = cm;
+        __syncthreads();
+        cm = period_sum<16>((lane & 15) < row_waves ? dots[side][wave0 + (lane & 15)] : 0.f);
+      }
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
         float x[8];
@@ -294,7 +328,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
-      if (here && piece(i) < pieces) store16(p.dx, row * pieces + piece(i), pack8(ds[i]));
+      if (here && piece(i) < pieces) store16(p.dx, row * pieces, piece(i), pack8(ds[i]));
   }
   // the row groups' column sums, in the groups' order, by the first of them
   auto put = [&](int at, const float(&d)[8], int v) {
@@ -302,15 +336,16 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
     float s[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] = d[e];
-    if constexpr (kGroups > 1) {
+    if (groups > 1) {
+      float* meet = reinterpret_cast<float*>(columns);
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) columns[e * kGradThreads + tid] = d[e];
+      for (int e = 0; e < 8; ++e) meet[e * kGradThreads + tid] = d[e];
       __syncthreads();
       if (group != 0) return;
-      for (int u = 1; u < kGroups; ++u)
+      for (int u = 1; u < groups; ++u)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = s[e] + columns[e * kGradThreads + u * 64 * kRowWaves + tid];
+        for (int e = 0; e < 8; ++e) s[e] = s[e] + meet[e * kGradThreads + u * 64 * row_waves + tid];
     }
     if (v >= pieces) return;
     float4* to = reinterpret_cast<float4*>(p.parts + (static_cast<int64_t>(at) * gridDim.x + blockIdx.x) * p.hidden) + 2 * v;
@@ -319,6 +354,14 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
   };
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
+    if constexpr (kVecs > 1) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const float4 a = held(0, i, half), b = held(1, i, half);
+        dpost[i][4 * half] = a.x, dpost[i][4 * half + 1] = a.y, dpost[i][4 * half + 2] = a.z, dpost[i][4 * half + 3] = a.w;
+        dgate[i][4 * half] = b.x, dgate[i][4 * half + 1] = b.y, dgate[i][4 * half + 2] = b.z, dgate[i][4 * half + 3] = b.w;
+      }
+    }
     put(p.pre_at, dpre[i], piece(i));
     put(p.post_at, dpost[i], piece(i));
     put(p.gate_at, dgate[i], piece(i));
@@ -360,13 +403,16 @@ __global__ __launch_bounds__(16 * kFoldSlots) void norm_fold_kernel(FoldParams p
   if (slot == 0 && col < p.hidden) *reinterpret_cast<float4*>(p.out[blockIdx.y] + col) = s;
 }
 
-// Rows a workgroup takes at a time.
-int grad_groups(int64_t hidden_dim) {
-  return hidden_dim <= 512 ? 16 : hidden_dim <= 1024 ? 8 : hidden_dim <= 2048 ? 4 : hidden_dim <= 4096 ? 2 : 1;
+// Pieces to a thread, and waves to a row.
+int grad_vecs(int64_t hidden_dim) { return hidden_dim <= 512 * kGradWaves ? 1 : 2; }
+int grad_row_waves(int64_t hidden_dim) {
+  const int64_t columns = 512 * grad_vecs(hidden_dim);
+  return static_cast<int>((hidden_dim + columns - 1) / columns);
 }
 
 int norm_sets(int64_t num_tokens, int64_t hidden_dim) {
-  const int64_t sets = (num_tokens + grad_groups(hidden_dim) - 1) / grad_groups(hidden_dim);
+  const int groups = kGradWaves / grad_row_waves(hidden_dim);
+  const int64_t sets = (num_tokens + groups - 1) / groups;
   return static_cast<int>(sets < kMaxSets ? sets : kMaxSets);
 }
 
@@ -433,23 +479,13 @@ hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hi
   p.post_at = sum_of(a.dpost_weight);
   p.gate_at = sum_of(a.gate_stride == 0 ? static_cast<float*>(a.dgate) : nullptr);
   if (f.sets > 0) {
-    auto launch = [&](auto row_waves, auto vecs) {
-      hipLaunchKernelGGL((residual_norm_grad_kernel<decltype(row_waves)::value, decltype(vecs)::value, decltype(vecs)::value == 1>), dim3(f.sets),
-                         dim3(kGradThreads), 0, stream, p);
-    };
-    using std::integral_constant;
-    const integral_constant<int, 1> one;
-    switch (grad_groups(a.hidden_dim)) {
-      case 16: launch(one, one); break;
-      case 8: launch(integral_constant<int, 2>{}, one); break;
-      case 4: launch(integral_constant<int, 4>{}, one); break;
-      case 2: launch(integral_constant<int, 8>{}, one); break;
-      default:
-        if (a.hidden_dim <= 8192)
-          launch(integral_constant<int, 16>{}, one);
-        else
-          launch(integral_constant<int, 16>{}, integral_constant<int, 2>{});
-    }
+    p.row_waves = grad_row_waves(a.hidden_dim);
+    p.groups = kGradWaves / p.row_waves;
+    const dim3 threads(64 * p.row_waves * p.groups);
+    if (grad_vecs(a.hidden_dim) == 1)
+      hipLaunchKernelGGL((residual_norm_grad_kernel<1, true>), dim3(f.sets), threads, 0, stream, p);
+    else
+      hipLaunchKernelGGL((residual_norm_grad_kernel<2, false>), dim3(f.sets), threads, 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

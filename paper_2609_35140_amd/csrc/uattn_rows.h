@@ -43,6 +43,14 @@ __device__ __forceinline__ void store16(void* p, int64_t piece, const u32x4& w) 
   reinterpret_cast<u32x4*>(p)[piece] = w;
 }
 
+// The same behind a base that is the wave's: scalar address, 32-bit offset in the lanes.
+__device__ __forceinline__ u32x4 load16(const void* base, int64_t uniform, uint32_t piece) {
+  return *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base) + 16 * uniform + 16u * piece);
+}
+__device__ __forceinline__ void store16(void* base, int64_t uniform, uint32_t piece, const u32x4& w) {
+  *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + 16 * uniform + 16u * piece) = w;
+}
+
 // DPP: every lane reads another of its 16; all lanes of the patterns used have a source.
 template <int ctrl>
 __device__ __forceinline__ float dpp_read(float x) {
