@@ -5,23 +5,29 @@
 //   x = z;  in the history: x = x > 0 ? x / repetition : x * repetition
 //   x = x - frequency * (times in the response);  in the response: x = x - presence
 //   x = x + bias (the last entry of the row's list that names v);  masked: x = -inf
-// in fp32, rounded to bf16 once.
+// in fp32 (the division as a product with 1 / repetition), rounded to bf16 once.
 //
-// A workgroup takes one stretch of kStretch entries of one row: it counts the
-// history's tokens that fall into the stretch in LDS (whole numbers, so the order
-// of the atomics does not show), then streams the stretch.  Nothing depends on the
-// other rows, so a decode step's row and the update's row of the same prefix get
-// the same bits.
+// A workgroup takes one stretch of kStretch entries of up to kMaxRows consecutive
+// rows.  It counts the history's tokens that fall into the stretch in LDS (whole
+// numbers, so the order of the atomics does not show) and streams the stretch.  Rows
+// of an update are successive prefixes of a sequence: where a row's history is the
+// one before it and some more, only the new tokens are counted, and most of them fall
+// into other stretches.  Counts do not depend on how they came about, so a decode
+// step's row and the update's row of the same prefix get the same bits.
+#include <type_traits>
+
 #include "uattn_internal.h"
 #include "uattn_rows.h"
 
 namespace uattn {
 namespace {
 
-constexpr int kLogitsThreads = 256;
-constexpr int kLogitsVecs = 4;
+constexpr int kLogitsThreads = 512;
+constexpr int kLogitsVecs = 2;
 constexpr int kStretch = kLogitsThreads * kLogitsVecs * 8;
+constexpr int kMaxRows = 16;
 constexpr uint32_t kPrompt = 0x80000000u;  // of a count: the entry occurs in the prompt
+constexpr int32_t kNoBias = INT32_MIN;     // of the bias table: as a float, -0, which changes no sum
 
 struct LogitsParams {
   const uint16_t* in;        // logits, or the processed logits' gradient
@@ -37,124 +43,203 @@ struct LogitsParams {
   const int32_t* mask_rows;  // [rows], or null: row t has mask t
   int64_t in_stride, logits_stride, out_stride, mask_stride;
   int32_t num_rows, vocab, num_tokens, num_bias, num_masks, stretches;
+  int32_t rows;   // consecutive rows to a workgroup
   int32_t first;  // workgroups of the launches before this one
 };
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return min(max(x, lo), hi); }
+__device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ float lane_float(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
 
-template <bool kGrad>
+template <bool kGrad, bool kBias>
 __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) {
   __shared__ uint32_t table[kStretch];
-  const int tid = threadIdx.x;
+  __shared__ int32_t bias_table[kBias ? kStretch : 1];
+  const int tid = threadIdx.x, lane = tid & 63;
   const int64_t unit = p.first + static_cast<int64_t>(blockIdx.x);
-  const int64_t row = unit / p.stretches;
+  const int64_t row0 = unit / p.stretches * p.rows;
   const int v0 = static_cast<int>(unit % p.stretches) * kStretch, n = min(kStretch, p.vocab - v0);
-  const uint16_t* in = p.in + row * p.in_stride + v0;
-  uint16_t* out = p.out + row * p.out_stride + v0;
+  const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows), p.num_rows - row0));
 
+  // Lane r of every wave keeps row r's arguments; the loops below read them from there.
+  int begin = 0, split = 0, end = 0, bias_begin = 0, bias_end = 0, mask_row = -1;
   float rep = 1.f, freq = 0.f, pres = 0.f;
-  int begin = 0, split = 0, end = 0;
-  if (p.history != nullptr) {
-    begin = clamp_int(p.history[3 * row], 0, p.num_tokens);
-    end = clamp_int(p.history[3 * row + 2], begin, p.num_tokens);
-    split = clamp_int(p.history[3 * row + 1], begin, end);
-    rep = p.penalties[3 * row];
-    freq = kGrad ? 0.f : p.penalties[3 * row + 1];
-    pres = kGrad ? 0.f : p.penalties[3 * row + 2];
+  if (lane < rows) {
+    const int64_t row = row0 + lane;
+    if (p.history != nullptr) {
+      begin = clamp_int(p.history[3 * row], 0, p.num_tokens);
+      split = p.history[3 * row + 1];
+      end = clamp_int(p.history[3 * row + 2], begin, p.num_tokens);
+      rep = p.penalties[3 * row];
+      if constexpr (!kGrad) {
+        freq = p.penalties[3 * row + 1];
+        pres = p.penalties[3 * row + 2];
+      }
+    }
+    if (kBias) {
+      bias_begin = clamp_int(p.bias_rows[2 * row], 0, p.num_bias);
+      bias_end = clamp_int(p.bias_rows[2 * row + 1], bias_begin, p.num_bias);
+    }
+    if (p.mask != nullptr) {
+      const int64_t m = p.mask_rows != nullptr ? p.mask_rows[row] : row;
+      mask_row = m >= 0 && m < p.num_masks ? static_cast<int>(m) : -1;
+    }
   }
-  // the prompt matters to the repetition penalty alone
-  if (rep == 1.f) begin = split;
-  if (rep == 1.f && freq == 0.f && pres == 0.f) end = begin;
-  int bias_begin = 0, bias_end = 0;
-  if (!kGrad && p.bias_rows != nullptr) {
-    bias_begin = clamp_int(p.bias_rows[2 * row], 0, p.num_bias);
-    bias_end = clamp_int(p.bias_rows[2 * row + 1], bias_begin, p.num_bias);
+  // a row's history goes on from the one before: the first of its new tokens; otherwise -1
+  int from = -1;
+  {
+    const int b = __shfl_up(begin, 1, 64), s = __shfl_up(split, 1, 64), e = __shfl_up(end, 1, 64);
+    if (lane > 0 && b == begin && s == split && e <= end) from = e;
   }
-  const uint32_t* mask = nullptr;
-  if (p.mask != nullptr) {
-    const int64_t m = p.mask_rows != nullptr ? p.mask_rows[row] : row;
-    if (m >= 0 && m < p.num_masks) mask = p.mask + m * p.mask_stride;
-  }
+  const int last_token = lane < rows && from >= 0 && end == from + 1 ? p.tokens[from] : -1;
+  const bool one_here = static_cast<uint32_t>(last_token) - v0 < static_cast<uint32_t>(n);
+  const bool active = begin < end && (rep != 1.f || freq != 0.f || pres != 0.f);
+  const uint64_t actives = __ballot(active);
+  const int bias_before = __shfl_up(bias_begin, 1, 64), bias_until = __shfl_up(bias_end, 1, 64);
+  const bool new_bias = lane == 0 || bias_before != bias_begin || bias_until != bias_end;
 
-  float x[kLogitsVecs][8];
+  auto load = [&](int r, u32x4 (&w)[kLogitsVecs], uint32_t (&keep)[kLogitsVecs]) {
+    const uint16_t* in = p.in + (row0 + r) * p.in_stride + v0;
+    const int m = lane_int(mask_row, r);
+    const uint8_t* mask = reinterpret_cast<const uint8_t*>(p.mask + m * p.mask_stride) + v0 / 8;
 #pragma unroll
-  for (int i = 0; i < kLogitsVecs; ++i) {
-    const int e0 = 8 * (tid + i * kLogitsThreads);
-    u32x4 w = {0, 0, 0, 0};
-    if (e0 + 8 <= n)
-      w = load16(in, e0 / 8);
-    else
-      for (int e = 0; e < n - e0; ++e) w[e / 2] |= static_cast<uint32_t>(in[e0 + e]) << (16 * (e & 1));
-    unpack8(w, x[i]);
-  }
-  auto clear = [&]() {
-    for (int e = tid; e < kStretch; e += kLogitsThreads) table[e] = 0;
-    __syncthreads();
+    for (int i = 0; i < kLogitsVecs; ++i) {
+      const int piece = tid + i * kLogitsThreads, e0 = 8 * piece;
+      w[i] = u32x4{0, 0, 0, 0};
+      keep[i] = 0xFF;
+      if (e0 + 8 <= n)
+        w[i] = load16(in, 0, piece);
+      else
+        for (int e = 0; e < n - e0; ++e) w[i][e / 2] |= static_cast<uint32_t>(in[e0 + e]) << (16 * (e & 1));
+      if (m >= 0 && e0 < n) keep[i] = mask[piece];
+    }
   };
-  if (begin < end) {
-    clear();
-    for (int i = begin + tid; i < end; i += kLogitsThreads) {
-      const uint32_t v = static_cast<uint32_t>(p.tokens[i]) - v0;
-      if (v < static_cast<uint32_t>(n)) {
-        if (i < split)
+  auto count = [&](int lo, int hi, int response) {
+    constexpr int kAhead = 4;
+    for (int i0 = lo + tid; i0 < hi; i0 += kAhead * kLogitsThreads) {
+      int token[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) token[u] = i0 + u * kLogitsThreads < hi ? p.tokens[i0 + u * kLogitsThreads] : -1;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const uint32_t v = static_cast<uint32_t>(token[u]) - v0;
+        if (v >= static_cast<uint32_t>(n)) continue;
+        if (i0 + u * kLogitsThreads < response)
           atomicOr(&table[v], kPrompt);
         else
           atomicAdd(&table[v], 1);
       }
     }
-    __syncthreads();
+  };
+
+  u32x4 next[kLogitsVecs];
+  uint32_t next_keep[kLogitsVecs];
+  load(0, next, next_keep);
+  for (int r = 0; r < rows; ++r) {
+    u32x4 w[kLogitsVecs];
+    uint32_t keep[kLogitsVecs];
 #pragma unroll
     for (int i = 0; i < kLogitsVecs; ++i) {
-      const int e0 = 8 * (tid + i * kLogitsThreads);
+      w[i] = next[i];
+      keep[i] = next_keep[i];
+    }
+    if (r + 1 < rows) load(r + 1, next, next_keep);
+    if (actives != 0) {
+      const int lo = lane_int(begin, r), hi = lane_int(end, r), response = lane_int(split, r), at = lane_int(from, r);
+      if (at < 0) {
+        __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t seen = table[e0 + e];
-        if (seen == 0) continue;
+        for (int e = 0; e < kStretch / 4; e += kLogitsThreads)
+          reinterpret_cast<u32x4*>(table)[e + tid] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        count(lo, hi, response);
+        __syncthreads();
+      } else if (hi - at > 1 || lane_int(one_here, r) != 0) {
+        __syncthreads();
+        count(at, hi, response);
+        __syncthreads();
+      }
+    }
+    if (kBias && lane_int(new_bias, r) != 0) {
+      const int lo = lane_int(bias_begin, r), hi = lane_int(bias_end, r);
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kStretch / 4; e += kLogitsThreads)
+        reinterpret_cast<u32x4*>(bias_table)[e + tid] = u32x4{kPrompt, kPrompt, kPrompt, kPrompt};
+      __syncthreads();
+      // the last entry that names v wins its place; then each place takes its winner's value
+      for (int i = lo + tid; i < hi; i += kLogitsThreads) {
+        const uint32_t v = static_cast<uint32_t>(p.bias_ids[i]) - v0;
+        if (v < static_cast<uint32_t>(n)) atomicMax(&bias_table[v], i);
+      }
+      __syncthreads();
+      for (int e = tid; e < kStretch; e += kLogitsThreads) {
+        const int32_t i = bias_table[e];
+        if (i != kNoBias) bias_table[e] = __float_as_int(p.bias_values[i]);
+      }
+      __syncthreads();
+    }
+    float x[kLogitsVecs][8];
+#pragma unroll
+    for (int i = 0; i < kLogitsVecs; ++i) unpack8(w[i], x[i]);
+    if (actives >> r & 1) {
+      const float mul = lane_float(rep, r), inv = 1.f / mul, f = lane_float(freq, r), q = lane_float(pres, r);
+      const uint16_t* z = p.logits + (row0 + r) * p.logits_stride + v0;
+#pragma unroll
+      for (int i = 0; i < kLogitsVecs; ++i) {
+        const int piece = tid + i * kLogitsThreads;
+        const u32x4 a = reinterpret_cast<const u32x4*>(table)[2 * piece], b = reinterpret_cast<const u32x4*>(table)[2 * piece + 1];
+        const uint32_t seen[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
         if constexpr (kGrad) {
-          const float z = bf16_lo(p.logits[row * p.logits_stride + v0 + e0 + e]);
-          x[i][e] = z > 0.f ? x[i][e] / rep : x[i][e] * rep;
+          if (((a[0] | a[1]) | (a[2] | a[3]) | (b[0] | b[1]) | (b[2] | b[3])) == 0) continue;
+          float zs[8];
+          if (8 * piece + 8 <= n) {
+            unpack8(load16(z, 0, piece), zs);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) zs[e] = 8 * piece + e < n ? bf16_lo(z[8 * piece + e]) : 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[i][e] = seen[e] == 0 ? x[i][e] : x[i][e] * (zs[e] > 0.f ? inv : mul);
         } else {
-          const uint32_t count = seen & ~kPrompt;
-          float y = x[i][e] > 0.f ? x[i][e] / rep : x[i][e] * rep;
-          if (count > 0) y = y - freq * static_cast<float>(count) - pres;
-          x[i][e] = y;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t times = seen[e] & ~kPrompt;
+            float y = x[i][e] * (x[i][e] > 0.f ? inv : mul);
+            y = __builtin_fmaf(-f, static_cast<float>(times), y) - (times != 0 ? q : 0.f);
+            x[i][e] = seen[e] == 0 ? x[i][e] : y;
+          }
         }
       }
     }
-  }
-  if (!kGrad && bias_begin < bias_end) {
-    __syncthreads();
-    clear();
-    for (int i = bias_begin + tid; i < bias_end; i += kLogitsThreads) {
-      const uint32_t v = static_cast<uint32_t>(p.bias_ids[i]) - v0;
-      if (v < static_cast<uint32_t>(n)) atomicMax(&table[v], static_cast<uint32_t>(i - bias_begin) + 1);
-    }
-    __syncthreads();
+    if (kBias && lane_int(bias_begin, r) < lane_int(bias_end, r)) {
 #pragma unroll
-    for (int i = 0; i < kLogitsVecs; ++i) {
-      const int e0 = 8 * (tid + i * kLogitsThreads);
+      for (int i = 0; i < kLogitsVecs; ++i) {
+        const float4* t = reinterpret_cast<const float4*>(bias_table) + 2 * (tid + i * kLogitsThreads);
+        const float4 a = t[0], b = t[1];
+        const float add[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t at = table[e0 + e];
-        if (at != 0) x[i][e] = x[i][e] + p.bias_values[bias_begin + at - 1];
+        for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] + add[e];
       }
     }
-  }
+    uint16_t* out = p.out + (row0 + r) * p.out_stride + v0;
+    const bool masked = lane_int(mask_row, r) >= 0;
 #pragma unroll
-  for (int i = 0; i < kLogitsVecs; ++i) {
-    const int e0 = 8 * (tid + i * kLogitsThreads);
-    if (e0 >= n) break;
-    if (mask != nullptr) {
-      const uint32_t keep = mask[(v0 + e0) / 32] >> ((v0 + e0) & 31);
+    for (int i = 0; i < kLogitsVecs; ++i) {
+      const int piece = tid + i * kLogitsThreads, e0 = 8 * piece;
+      if (e0 >= n) break;
+      if (masked) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (!(keep >> e & 1)) x[i][e] = kGrad ? 0.f : -__builtin_inff();
+        for (int e = 0; e < 8; ++e) x[i][e] = keep[i] >> e & 1 ? x[i][e] : (kGrad ? 0.f : -__builtin_inff());
+      }
+      const u32x4 o = pack8(x[i]);
+      if (e0 + 8 <= n)
+        store16(out, 0, piece, o);
+      else
+        for (int e = 0; e < n - e0; ++e) out[e0 + e] = static_cast<uint16_t>(o[e / 2] >> (16 * (e & 1)));
     }
-    const u32x4 w = pack8(x[i]);
-    if (e0 + 8 <= n)
-      store16(out, e0 / 8, w);
-    else
-      for (int e = 0; e < n - e0; ++e) out[e0 + e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
   }
 }
 
@@ -181,12 +266,18 @@ hipError_t launch_logits(const LogitsLaunch& a, bool grad, hipStream_t stream) {
   p.num_bias = a.num_bias;
   p.num_masks = a.num_masks;
   p.stretches = (a.vocab - 1) / kStretch + 1;
-  return launch_parts(static_cast<int64_t>(a.num_rows) * p.stretches, kLogitsThreads, [&](int first, unsigned n) {
+  // few rows are spread over all CUs, many share their counts
+  const int64_t share = static_cast<int64_t>(a.num_rows) * p.stretches / (16 * device_cus());
+  p.rows = static_cast<int>(share < 1 ? 1 : share > kMaxRows ? kMaxRows : share);
+  const int64_t groups = (static_cast<int64_t>(a.num_rows) + p.rows - 1) / p.rows;
+  return launch_parts(groups * p.stretches, kLogitsThreads, [&](int first, unsigned n) {
     p.first = first;
     if (grad)
-      hipLaunchKernelGGL(logits_kernel<true>, dim3(n), dim3(kLogitsThreads), 0, stream, p);
+      hipLaunchKernelGGL((logits_kernel<true, false>), dim3(n), dim3(kLogitsThreads), 0, stream, p);
+    else if (a.bias_rows != nullptr)
+      hipLaunchKernelGGL((logits_kernel<false, true>), dim3(n), dim3(kLogitsThreads), 0, stream, p);
     else
-      hipLaunchKernelGGL(logits_kernel<false>, dim3(n), dim3(kLogitsThreads), 0, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, false>), dim3(n), dim3(kLogitsThreads), 0, stream, p);
   });
 }
 

@@ -137,6 +137,53 @@ def test_same_id_twice_in_a_bias_list(ua):
         assert got[0, 5] == 4 and got[0, 9] == 5 and got[1, 5] == 3 and got[1, 9] == 2 and np.count_nonzero(got) == 4
 
 
+def test_earlier_entry_does_not_win_over_a_value_like_its_place(ua):
+    """The last entry's value is 0.0, or the number whose bits are an earlier entry's place in the list."""
+    V = 16
+    z = _rows(np.full((2, V), 0x3F80, dtype=np.uint16))[:, :V]
+    vals = np.array([7.0, 0.0, 8.0, 9.0, 0.0], dtype=np.float32)
+    vals[4] = np.array([2], dtype=np.int32).view(np.float32)[0]
+    got = gu.host_f64(ua.logits_process(z, bias_ids=gu.dev_i32([5, 5, 6, 6, 6]), bias_values=_f32(vals),
+                                        bias_rows=gu.dev_i32([[0, 5], [0, 4]])))
+    assert got[0, 5] == 1 and got[0, 6] == 1 and got[1, 5] == 1 and got[1, 6] == 10
+
+
+@pytest.mark.parametrize("T,V", [(700, 20011), (90, 151936)])
+def test_histories_that_go_on_from_row_to_row(ua, T, V):
+    """Many rows whose histories grow by none, one or several tokens, change their sequence, or shrink: what a row alone gets."""
+    import torch
+    g = inputs.rng(344, T)
+    tok = np.minimum(np.exp(g.random(9000) * np.log(V)).astype(np.int64) - 1, V - 1)
+    hist, b, s, e = [], 0, 40, 3
+    for t in range(T):
+        k = g.integers(0, 20)
+        if k == 0:
+            b = int(g.integers(0, 4000))
+            s, e = b + int(g.integers(0, 60)), b + int(g.integers(0, 90))
+        elif k == 1:
+            e = max(b, e - 5)
+        elif k == 2:
+            s += 1
+        else:
+            e += int(g.choice([0, 1, 1, 1, 1, 2, 700], p=[0.1, 0.2, 0.2, 0.2, 0.2, 0.08, 0.02]))
+        hist.append((b, s, min(e, 9000)))
+    pen = np.stack([1 + g.random(T), g.random(T), g.random(T)], 1)
+    pen[g.random(T) < 0.2] = (1, 0, 0)
+    bias_rows = np.repeat(np.stack([np.arange(T // 7 + 1) * 3, np.arange(T // 7 + 1) * 3 + 5], 1), 7, axis=0)[:T]
+    M = int(bias_rows.max())
+    one = dict(tokens=gu.dev_i32(tok), bias_ids=gu.dev_i32(g.integers(0, V, M)), bias_values=_f32(g.standard_normal(M)))
+    z = _rows(inputs.normal_bf16((T, V), 2.0, 345))[:, :V]
+    h, p, br = gu.dev_i32(hist), _f32(pen), gu.dev_i32(bias_rows)
+    full = ua.logits_process(z, history=h, penalties=p, bias_rows=br, **one)
+    back = ua.logits_process_backward(full, z, tokens=one["tokens"], history=h, penalties=p)
+    for t in range(0, T, 1 if T < 100 else 13):
+        at = slice(t, t + 1)
+        row = ua.logits_process(z[at], history=h[at], penalties=p[at], bias_rows=br[at], **one)
+        assert torch.equal(row.view(torch.int16), full[at].view(torch.int16)), t
+        row = ua.logits_process_backward(full[at], z[at], tokens=one["tokens"], history=h[at], penalties=p[at])
+        assert torch.equal(row.view(torch.int16), back[at].view(torch.int16)), t
+
+
 def test_update_rows_equal_decode_rows(ua):
     """A packed sequence's rows in one call, and each as the decode step at its position processes it: the same bits, and
     the same log-probability."""
