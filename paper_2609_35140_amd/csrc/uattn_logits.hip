@@ -55,8 +55,9 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
 
 template <bool kGrad, bool kBias>
 __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) {
-  __shared__ uint32_t table[kStretch];
-  __shared__ int32_t bias_table[kBias ? kStretch : 1];
+  // counts, and behind them the biases (in their place where the counts serve one row alone)
+  extern __shared__ __align__(16) uint32_t table[];
+  int32_t* bias_table = reinterpret_cast<int32_t*>(table) + (p.rows > 1 ? kStretch : 0);
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t unit = p.first + static_cast<int64_t>(blockIdx.x);
   const int64_t row0 = unit / p.stretches * p.rows;
@@ -134,6 +135,21 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
     }
   };
 
+  // Backward: the logits of the pieces that hold entries of the history, and which of the next row's are here already
+  // (those that this row's counts ask for; a row's own new ones are read when its counts are known).
+  u32x4 next_z[kLogitsVecs];
+  bool have_z[kLogitsVecs] = {};
+  auto load_z = [&](int r, int i) {
+    const int piece = tid + i * kLogitsThreads;
+    const uint16_t* z = p.logits + (row0 + r) * p.logits_stride + v0;
+    u32x4 q = {0, 0, 0, 0};
+    if (8 * piece + 8 <= n)
+      q = load16(z, 0, piece);
+    else
+      for (int e = 0; e < n - 8 * piece; ++e) q[e / 2] |= static_cast<uint32_t>(z[8 * piece + e]) << (16 * (e & 1));
+    return q;
+  };
+
   u32x4 next[kLogitsVecs];
   uint32_t next_keep[kLogitsVecs];
   load(0, next, next_keep);
@@ -144,6 +160,12 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
     for (int i = 0; i < kLogitsVecs; ++i) {
       w[i] = next[i];
       keep[i] = next_keep[i];
+    }
+    // a thread's first bias, asked for before the counts
+    int first_id = -1;
+    if (kBias && lane_int(new_bias, r) != 0) {
+      const int i = lane_int(bias_begin, r) + tid;
+      if (i < lane_int(bias_end, r)) first_id = p.bias_ids[i];
     }
     if (r + 1 < rows) load(r + 1, next, next_keep);
     if (actives != 0) {
@@ -162,48 +184,48 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
         __syncthreads();
       }
     }
-    if (kBias && lane_int(new_bias, r) != 0) {
-      const int lo = lane_int(bias_begin, r), hi = lane_int(bias_end, r);
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < kStretch / 4; e += kLogitsThreads)
-        reinterpret_cast<u32x4*>(bias_table)[e + tid] = u32x4{kPrompt, kPrompt, kPrompt, kPrompt};
-      __syncthreads();
-      // the last entry that names v wins its place; then each place takes its winner's value
-      for (int i = lo + tid; i < hi; i += kLogitsThreads) {
-        const uint32_t v = static_cast<uint32_t>(p.bias_ids[i]) - v0;
-        if (v < static_cast<uint32_t>(n)) atomicMax(&bias_table[v], i);
-      }
-      __syncthreads();
-      for (int e = tid; e < kStretch; e += kLogitsThreads) {
-        const int32_t i = bias_table[e];
-        if (i != kNoBias) bias_table[e] = __float_as_int(p.bias_values[i]);
-      }
-      __syncthreads();
-    }
     float x[kLogitsVecs][8];
 #pragma unroll
     for (int i = 0; i < kLogitsVecs; ++i) unpack8(w[i], x[i]);
     if (actives >> r & 1) {
       const float mul = lane_float(rep, r), inv = 1.f / mul, f = lane_float(freq, r), q = lane_float(pres, r);
-      const uint16_t* z = p.logits + (row0 + r) * p.logits_stride + v0;
+      auto counts = [&](int i, uint32_t (&seen)[8]) {
+        const u32x4* t = reinterpret_cast<const u32x4*>(table) + 2 * (tid + i * kLogitsThreads);
+        const u32x4 a = t[0], b = t[1];
+        uint32_t any = 0;
 #pragma unroll
-      for (int i = 0; i < kLogitsVecs; ++i) {
-        const int piece = tid + i * kLogitsThreads;
-        const u32x4 a = reinterpret_cast<const u32x4*>(table)[2 * piece], b = reinterpret_cast<const u32x4*>(table)[2 * piece + 1];
-        const uint32_t seen[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        if constexpr (kGrad) {
-          if (((a[0] | a[1]) | (a[2] | a[3]) | (b[0] | b[1]) | (b[2] | b[3])) == 0) continue;
+        for (int e = 0; e < 4; ++e) {
+          seen[e] = a[e];
+          seen[e + 4] = b[e];
+          any |= a[e] | b[e];
+        }
+        return any != 0;
+      };
+      if constexpr (kGrad) {
+        uint32_t seen[kLogitsVecs][8];
+        u32x4 z[kLogitsVecs];
+#pragma unroll
+        for (int i = 0; i < kLogitsVecs; ++i) {
+          const bool hit = counts(i, seen[i]);
+          z[i] = next_z[i];
+          if (hit && !have_z[i]) z[i] = load_z(r, i);
+          have_z[i] = hit && r + 1 < rows;
+        }
+#pragma unroll
+        for (int i = 0; i < kLogitsVecs; ++i)
+          if (have_z[i]) next_z[i] = load_z(r + 1, i);
+#pragma unroll
+        for (int i = 0; i < kLogitsVecs; ++i) {
           float zs[8];
-          if (8 * piece + 8 <= n) {
-            unpack8(load16(z, 0, piece), zs);
-          } else {
+          unpack8(z[i], zs);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) zs[e] = 8 * piece + e < n ? bf16_lo(z[8 * piece + e]) : 0.f;
-          }
+          for (int e = 0; e < 8; ++e) x[i][e] = seen[i][e] == 0 ? x[i][e] : x[i][e] * (zs[e] > 0.f ? inv : mul);
+        }
+      } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[i][e] = seen[e] == 0 ? x[i][e] : x[i][e] * (zs[e] > 0.f ? inv : mul);
-        } else {
+        for (int i = 0; i < kLogitsVecs; ++i) {
+          uint32_t seen[8];
+          if (!counts(i, seen)) continue;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const uint32_t times = seen[e] & ~kPrompt;
@@ -213,6 +235,28 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
           }
         }
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLogitsVecs; ++i) have_z[i] = false;
+    }
+    if (kBias && lane_int(new_bias, r) != 0) {
+      const int lo = lane_int(bias_begin, r), hi = lane_int(bias_end, r);
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kStretch / 4; e += kLogitsThreads)
+        reinterpret_cast<u32x4*>(bias_table)[e + tid] = u32x4{kPrompt, kPrompt, kPrompt, kPrompt};
+      __syncthreads();
+      // the last entry that names v wins its place; then each place takes its winner's value
+      for (int i = lo + tid; i < hi; i += kLogitsThreads) {
+        const uint32_t v = static_cast<uint32_t>(i == lo + tid ? first_id : p.bias_ids[i]) - v0;
+        if (v < static_cast<uint32_t>(n)) atomicMax(&bias_table[v], i);
+      }
+      __syncthreads();
+      for (int e = tid; e < kStretch; e += kLogitsThreads) {
+        const int32_t i = bias_table[e];
+        if (i != kNoBias) bias_table[e] = __float_as_int(p.bias_values[i]);
+      }
+      __syncthreads();
     }
     if (kBias && lane_int(bias_begin, r) < lane_int(bias_end, r)) {
 #pragma unroll
@@ -270,14 +314,15 @@ hipError_t launch_logits(const LogitsLaunch& a, bool grad, hipStream_t stream) {
   const int64_t share = static_cast<int64_t>(a.num_rows) * p.stretches / (16 * device_cus());
   p.rows = static_cast<int>(share < 1 ? 1 : share > kMaxRows ? kMaxRows : share);
   const int64_t groups = (static_cast<int64_t>(a.num_rows) + p.rows - 1) / p.rows;
+  const size_t lds = sizeof(uint32_t) * kStretch * (a.bias_rows != nullptr && p.rows > 1 ? 2 : 1);
   return launch_parts(groups * p.stretches, kLogitsThreads, [&](int first, unsigned n) {
     p.first = first;
     if (grad)
-      hipLaunchKernelGGL((logits_kernel<true, false>), dim3(n), dim3(kLogitsThreads), 0, stream, p);
+      hipLaunchKernelGGL((logits_kernel<true, false>), dim3(n), dim3(kLogitsThreads), lds, stream, p);
     else if (a.bias_rows != nullptr)
-      hipLaunchKernelGGL((logits_kernel<false, true>), dim3(n), dim3(kLogitsThreads), 0, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, true>), dim3(n), dim3(kLogitsThreads), lds, stream, p);
     else
-      hipLaunchKernelGGL((logits_kernel<false, false>), dim3(n), dim3(kLogitsThreads), 0, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, false>), dim3(n), dim3(kLogitsThreads), lds, stream, p);
   });
 }
 
