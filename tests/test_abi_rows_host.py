@@ -112,6 +112,6 @@ def test_workspace_bytes(lib):
     assert g(0, 64) == g(-1, 64) == g(4, 0) == 0
     # three sums of a group of rows each; they stop growing with the tokens
     assert f(1, 64) == 3 * 64 * 4 and f(100000, 4096) == f(1 << 30, 4096)
-    # sorted keys and order, and for every 64 tokens two fp32 rows of partial sums
-    assert 16 * 4096 + 2 * 64 * 1024 * 4 <= g(4096, 1024) <= 64 * 4096 + 2 * 64 * 1024 * 4 + (1 << 20)
+    # sorted keys and order, and for every 32 tokens two fp32 rows of partial sums
+    assert 16 * 4096 + 2 * 128 * 1024 * 4 <= g(4096, 1024) <= 64 * 4096 + 2 * 128 * 1024 * 4 + (1 << 20)
     assert g(1 << 30, 8) > 1 << 32
