@@ -3,8 +3,8 @@
 // Lookup: out[t] = bf16(scale * table[ids[t]]), a wave to a token's row.
 //
 // Gradient: grad[v] = scale * (sum of dout[t] over the tokens t with ids[t] = v).
-// The tokens are sorted by id, stably (a radix sort of up to 9 bits a pass), so that an
-// entry's tokens stand together and in ascending order.  An entry's run is cut
+// The tokens are sorted by id, stably, so that an entry's tokens stand together and in
+// ascending order.  An entry's run is cut
 // into pieces of kPiece tokens counted from the run's own first one; a wave sums
 // one piece over 512 columns, in order, in fp32; runs of one piece are written at
 // once, the pieces of longer ones meet in the workspace and are added in order.
@@ -67,58 +67,35 @@ __global__ __launch_bounds__(kEmbedWaves * 64) void embedding_kernel(EmbeddingPa
 }
 
 // ---------------------------------------------------------------------------
-// Sorting, and zeros for the rows without a token beside it
+// Sorting, and zeros for the table beside it
 // ---------------------------------------------------------------------------
-constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;  // of a pass of the sort, at most
+constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;  // of a pass of a radix sort, at most
 constexpr int kPiece = 32;                 // tokens a wave sums
-constexpr int kPieceOfLong = 1 << 30;      // of a piece's length: the run is longer than a piece
-// Up to kSmall tokens one workgroup sorts them in LDS (a launch instead of five); it takes about as
-// long as five small launches there, and runs beside the zeros where these are asked for.
-constexpr int kSmall = 16384, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+// Up to kSmall tokens are sorted in one launch, by kBuckets workgroups in LDS: the b-th takes the ids
+// v with v % kBuckets = b, so that frequent neighbours are spread.  (One workgroup for all: 16,000
+// tokens 62 us.  The launches for more tokens take about 40, whatever their number up to 65,536.)
+constexpr int kSmall = 16384, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kBuckets = 32;
 constexpr int kSmallRounds = kSmall / kSmallThreads;
 constexpr int kTileThreads = 512, kTileWaves = kTileThreads / 64;
 constexpr int kTile = 2048, kTileRounds = kTile / kTileThreads;
 
-// The zeros of a launch: rows [begin, end) of the gradient that no id names, 16-byte pieces.
+// The zeros of a launch: rows [begin, end) of the gradient, 16-byte pieces.  Rows that have tokens are
+// cleared too: to find the others, every workgroup would read all ids, which costs about as much.
 struct ZeroParams {
   void* grad;
-  const int32_t* ids;
   int64_t row_pieces;  // from row to row
   int32_t pieces;      // of a row
-  int32_t num_tokens, begin, end;
+  int32_t begin, end;
   int32_t sorters;     // workgroups of the launch that sort; the others write zeros
 };
 
-// By a workgroup of kThreads threads, the `part`-th of `parts`: it marks the rows of its share that have
-// a token and clears the others.
+// By a workgroup of kThreads threads, the `part`-th of `parts`, a wave to a row.
 template <int kThreads>
-__device__ __forceinline__ void zero_rows(const ZeroParams& z, int part, int parts, uint32_t* marks) {
-  constexpr int kRows = 4096;  // marked at a time
-  const int64_t rows = z.end - z.begin;
-  const int64_t first = z.begin + rows * part / parts, last = z.begin + rows * (part + 1) / parts;
+__device__ __forceinline__ void zero_rows(const ZeroParams& z, int part, int parts) {
+  constexpr int kWaves = kThreads / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int64_t r0 = first; r0 < last; r0 += kRows) {
-    const uint32_t n = static_cast<uint32_t>(last - r0 < kRows ? last - r0 : kRows);
-    for (int i = threadIdx.x; i < kRows / 32; i += kThreads) marks[i] = 0;
-    __syncthreads();
-    constexpr int kAhead = 8;
-    for (int64_t i0 = threadIdx.x; i0 < z.num_tokens; i0 += kAhead * kThreads) {
-      int32_t id[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) id[u] = i0 + u * kThreads < z.num_tokens ? z.ids[i0 + u * kThreads] : -1;
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const uint32_t r = static_cast<uint32_t>(id[u]) - static_cast<uint32_t>(r0);
-        if (r < n) atomicOr(&marks[r / 32], 1u << (r & 31));
-      }
-    }
-    __syncthreads();
-    for (uint32_t r = wave; r < n; r += kThreads / 64) {
-      if (marks[r / 32] >> (r & 31) & 1) continue;
-      for (int v = lane; v < z.pieces; v += 64) store16(z.grad, (r0 + r) * z.row_pieces, v, u32x4{0, 0, 0, 0});
-    }
-    __syncthreads();
-  }
+  for (int64_t r = z.begin + static_cast<int64_t>(part) * kWaves + wave; r < z.end; r += static_cast<int64_t>(parts) * kWaves)
+    for (int v = lane; v < z.pieces; v += 64) store16(z.grad, r * z.row_pieces, v, u32x4{0, 0, 0, 0});
 }
 
 // Ids outside [0, vocab) have no row: they sort behind all others.
@@ -166,36 +143,115 @@ __device__ __forceinline__ int32_t scan_bins(int32_t x, int32_t* wave_totals) {
   return before + s - x;
 }
 
-// The first position in [lo, hi) whose key is above `key - !after`: the run's start or its end.
-__device__ __forceinline__ int run_bound(const uint32_t* keys, int lo, int hi, uint32_t key, bool after) {
-  while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    if (keys[mid] < key || (after && keys[mid] == key))
-      lo = mid + 1;
-    else
-      hi = mid;
+// The first of the `n` ascending keys that is not below `key`, by a wave: 64 probes a step.
+__device__ __forceinline__ int wave_lower_bound(const uint32_t* keys, int n, uint32_t key) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  while (n > 0) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const int below = __popcll(__ballot(at < n && keys[lo + at] < key));
+    if (below == 0) return lo;
+    lo += (below - 1) * step + 1;
+    n = min(step - 1, n - (below - 1) * step - 1);
   }
   return lo;
 }
 
-// Whether sorted position i begins a piece (a multiple of kPiece behind its run's start), its length
-// with kPieceOfLong, and whether it is the first of a run of several.
-struct PieceAt {
-  int length;  // 0: no piece begins here
-  bool first_of_long;
+// A piece: what one wave sums over 512 columns.
+struct Piece {
+  int32_t at;      // its first sorted position
+  int32_t tokens;  // up to kPiece, with the marks below
+  uint32_t row;    // of the gradient
+  int32_t token;   // the first
 };
-__device__ __forceinline__ PieceAt piece_at(const uint32_t* keys, int num_tokens, int32_t vocab, int i) {
-  const uint32_t key = keys[i];
-  if (key >= static_cast<uint32_t>(vocab)) return {0, false};
-  const bool first = i == 0 || keys[i - 1] != key;
-  if (!first) {
-    if (i < kPiece || keys[i - kPiece] != key) return {0, false};
-    if ((i - run_bound(keys, 0, i, key, false)) % kPiece != 0) return {0, false};
+constexpr int kOfLong = 1 << 30;   // its run is longer than a piece: the sum is a part
+constexpr int kFirst = 1 << 29;    // ... the run's first
+struct LongRun {
+  int32_t begin, end;  // sorted positions
+  uint32_t row;
+};
+
+// Lists the pieces that begin at the wave's 64 sorted positions i0 + lane of `n`, whose keys ascend up to
+// `limit` (keys from there on have no row): every position a multiple of kPiece behind its run's start.
+// order(i) and row(key) name position i's token and a key's row; sorted positions count from `base` on in the lists.
+// pieces and longs are counted in counts[0] and counts[1].
+template <class Order, class Row>
+__device__ __forceinline__ void list_pieces(const uint32_t* keys, int n, uint32_t limit, int i0, int base, const Order& order,
+                                            const Row& row, int32_t* counts, Piece* pieces, LongRun* longs) {
+  const int lane = threadIdx.x & 63, i = i0 + lane;
+  // the starts of runs at the positions from i0 on: 64, and 32 behind them (positions from n on count as starts)
+  const uint32_t key = i < n ? keys[i] : limit;
+  const bool start = i >= n || i == 0 || keys[i - 1] != key;
+  const uint64_t starts = __ballot(start);
+  const int j = i0 + 64 + lane;
+  const uint64_t behind = __ballot(lane < kPiece + 1 && (j >= n || keys[j - 1] != keys[j]));
+  // the run of the positions before the wave's first start
+  int before = i0;
+  if ((starts & 1) == 0) {
+    const uint32_t first = __builtin_amdgcn_readfirstlane(key);
+    before = wave_lower_bound(keys, i0, first);
   }
-  const int n = run_bound(keys, i, min(i + kPiece, num_tokens), key, true) - i;
-  const bool goes_on = i + n < num_tokens && keys[i + n] == key;
-  return {!first || goes_on ? n | kPieceOfLong : n, first && goes_on};
+  const uint64_t until = starts & (~uint64_t{0} >> (63 - lane));  // starts at this lane or before
+  const int begin = until != 0 ? i0 + 63 - __clzll(static_cast<long long>(until)) : before;
+  if (i >= n || key >= limit || (i - begin) % kPiece != 0) return;
+  // positions to the next start, up to kPiece + 1
+  const uint64_t later = lane == 63 ? behind : (starts >> (lane + 1)) | (behind << (63 - lane));
+  const int run = later != 0 ? __ffsll(static_cast<unsigned long long>(later)) : kPiece + 1;
+  const bool goes_on = run > kPiece, is_first = i == begin;
+  int tokens = goes_on ? kPiece : run;
+  if (goes_on || !is_first) tokens |= kOfLong | (is_first ? kFirst : 0);
+  pieces[atomicAdd(&counts[0], 1)] = Piece{base + i, tokens, row(key), order(i)};
+  // the run's last piece names the run
+  if (!goes_on && !is_first) longs[atomicAdd(&counts[1], 1)] = LongRun{base + begin, base + i + run, row(key)};
 }
+
+// The lists have a part to a bucket (all in the first where there are none): its pieces begin at the
+// bucket's first sorted position, its long runs at a kPiece-th of it (they are longer than kPiece).
+struct ListHeads {
+  int32_t pieces[kBuckets], longs[kBuckets], base[kBuckets];
+};
+
+// The lists' parts as a wave reads them: lane b keeps the b-th's.
+struct ListParts {
+  int32_t until, count, base;
+  __device__ __forceinline__ ListParts(const int32_t* counts, const int32_t* bases, int divide) {
+    const int lane = threadIdx.x & 63;
+    count = lane < kBuckets ? counts[lane] : 0;
+    base = lane < kBuckets ? bases[lane] / divide : 0;
+    until = count;
+#pragma unroll
+    for (int d = 1; d < kBuckets; d *= 2) {
+      const int32_t y = __shfl_up(until, d, 64);
+      if (lane >= d) until += y;
+    }
+  }
+  __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(until, kBuckets - 1); }
+  // where the k-th entry of all stands
+  __device__ __forceinline__ int at(int k) const {
+    const int b = __popcll(__ballot((threadIdx.x & 63) < kBuckets && until <= k));
+    return k - __builtin_amdgcn_readlane(until, b) + __builtin_amdgcn_readlane(count, b) + __builtin_amdgcn_readlane(base, b);
+  }
+};
+
+// Walks (entry, block of 512 columns) pairs, entries outside, `step` pairs at a time, without divisions.
+struct PairWalk {
+  int32_t entry, block, blocks, entry_step, block_step;
+  __device__ __forceinline__ PairWalk(int32_t first, int32_t step, int32_t columns) {
+    blocks = (columns + 511) / 512;
+    entry = first / blocks;
+    block = first % blocks;
+    entry_step = step / blocks;
+    block_step = step % blocks;
+  }
+  __device__ __forceinline__ void go_on() {
+    entry += entry_step;
+    block += block_step;
+    if (block >= blocks) {
+      block -= blocks;
+      ++entry;
+    }
+  }
+};
 
 struct SortParams {
   const int32_t* ids;            // the first pass reads these, the others keys_in and order_in
@@ -204,81 +260,116 @@ struct SortParams {
   uint32_t* keys_out;
   int32_t* order_out;
   int32_t* hist;                 // [tiles][kBins]
-  int32_t* counts;               // pieces, runs of several
-  int2* pieces;                  // first sorted position, tokens (| kPieceOfLong)
-  int32_t* longs;                // first sorted position
+  ListHeads* heads;
+  Piece* pieces;
+  LongRun* longs;
   int32_t num_tokens, vocab, tiles, shift, bits;  // of the digit
   int32_t passes;
   ZeroParams zero;
 };
 
-// All passes and the list of pieces for up to kSmall tokens, by workgroup 0.  A wave's tokens are
-// consecutive, 64 to a round; in a pass each gets its place among the wave's of its digit, the counts
-// of (digit, wave) are summed, and the tokens move.
+// A bucket of up to kSmall tokens, sorted and listed.  A wave's tokens are consecutive, 64 to a round; in
+// a pass each gets its place among the wave's of its digit, the counts of (digit, wave) are summed, and
+// the tokens move.
 __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p) {
-  __shared__ uint32_t keys[kSmall];
-  __shared__ uint16_t order[kSmall];
+  extern __shared__ __align__(16) uint32_t keys[];  // [num_tokens] and as many 16-bit orders
   __shared__ int32_t seen[kSmallWaves][kBins];
-  __shared__ int32_t base[kBins], wave_totals[kBins / 64], counts[2];
+  __shared__ int32_t first_of[kBins], wave_totals[kBins / 64], mine_of[kSmallWaves], before_of[kSmallWaves], counts[2];
   if (static_cast<int>(blockIdx.x) >= p.zero.sorters) {
-    zero_rows<kSmallThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters, keys);
+    zero_rows<kSmallThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters);
     return;
   }
+  uint16_t* order = reinterpret_cast<uint16_t*>(keys + p.num_tokens);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rounds = (p.num_tokens + kSmallThreads - 1) / kSmallThreads, begin = wave * rounds * 64 + lane;
+  const uint64_t below = (uint64_t{1} << lane) - 1;
+  int rounds = (p.num_tokens + kSmallThreads - 1) / kSmallThreads, begin = wave * rounds * 64 + lane;
   uint32_t key[kSmallRounds];
   int32_t from[kSmallRounds], at[kSmallRounds];
+  // the bucket's tokens, in order, and the number of tokens in the buckets before it
+  int mine = 0, before = 0;
 #pragma unroll
   for (int r = 0; r < kSmallRounds; ++r) {
-    from[r] = begin + r * 64;
-    key[r] = r < rounds && from[r] < p.num_tokens ? sort_key(p.ids[from[r]], p.vocab) : 0;
+    key[r] = p.vocab;
+    if (r < rounds && begin + r * 64 < p.num_tokens) key[r] = sort_key(p.ids[begin + r * 64], p.vocab);
+  }
+#pragma unroll
+  for (int r = 0; r < kSmallRounds; ++r) {
+    if (r >= rounds) break;
+    const bool valid = key[r] < static_cast<uint32_t>(p.vocab);
+    mine += __popcll(__ballot(valid && key[r] % kBuckets == blockIdx.x));
+    before += __popcll(__ballot(valid && key[r] % kBuckets < blockIdx.x));
+  }
+  if (lane == 0) {
+    mine_of[wave] = mine;
+    before_of[wave] = before;
   }
   if (tid < 2) counts[tid] = 0;
+  __syncthreads();
+  int n = 0, base = 0, to = 0;
+#pragma unroll
+  for (int w = 0; w < kSmallWaves; ++w) {
+    if (w == wave) to = n;
+    n += mine_of[w];
+    base += before_of[w];
+  }
+#pragma unroll
+  for (int r = 0; r < kSmallRounds; ++r) {
+    if (r >= rounds) break;
+    const bool here = key[r] < static_cast<uint32_t>(p.vocab) && key[r] % kBuckets == blockIdx.x;
+    const uint64_t all = __ballot(here);
+    if (here) {
+      keys[to + __popcll(all & below)] = key[r] / kBuckets;
+      order[to + __popcll(all & below)] = static_cast<uint16_t>(begin + r * 64);
+    }
+    to += __popcll(all);
+  }
+  rounds = (n + kSmallThreads - 1) / kSmallThreads;
+  begin = wave * rounds * 64 + lane;
   for (int pass = 0; pass < p.passes; ++pass) {
-    const int shift = pass * p.bits;
-    const uint32_t low = (1u << p.bits) - 1;
+    const int shift = pass * p.bits, bins = 1 << p.bits;
+    const uint32_t low = bins - 1;
     for (int i = tid; i < kSmallWaves * kBins; i += kSmallThreads) seen[0][i] = 0;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSmallRounds; ++r)
-      if (r < rounds) at[r] = rank_in_wave(seen[wave], key[r] >> shift & low, begin + r * 64 < p.num_tokens, p.bits, lane);
+    for (int r = 0; r < kSmallRounds; ++r) {
+      if (r >= rounds) break;
+      const int i = begin + r * 64;
+      key[r] = i < n ? keys[i] : 0;
+      from[r] = i < n ? order[i] : 0;
+      at[r] = rank_in_wave(seen[wave], key[r] >> shift & low, i < n, p.bits, lane);
+    }
     __syncthreads();
     int32_t all = 0;
-    if (tid < kBins)
+    if (tid < bins)
       for (int w = 0; w < kSmallWaves; ++w) {
-        const int32_t n = seen[w][tid];
+        const int32_t c = seen[w][tid];
         seen[w][tid] = all;
-        all += n;
+        all += c;
       }
-    const int32_t before = scan_bins(all, wave_totals);
-    if (tid < kBins) base[tid] = before;
+    const int32_t smaller = scan_bins(all, wave_totals);
+    if (tid < kBins) first_of[tid] = smaller;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSmallRounds; ++r) {
-      if (r >= rounds || begin + r * 64 >= p.num_tokens) continue;
+      if (r >= rounds || begin + r * 64 >= n) break;
       const uint32_t digit = key[r] >> shift & low;
-      const int to = base[digit] + seen[wave][digit] + at[r];
-      keys[to] = key[r];
-      order[to] = static_cast<uint16_t>(from[r]);
+      const int place = first_of[digit] + seen[wave][digit] + at[r];
+      keys[place] = key[r];
+      order[place] = static_cast<uint16_t>(from[r]);
     }
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSmallRounds; ++r) {
-      const int i = begin + r * 64;
-      if (r >= rounds || i >= p.num_tokens) continue;
-      key[r] = keys[i];
-      from[r] = order[i];
-    }
   }
-  for (int i = tid; i < p.num_tokens; i += kSmallThreads) {
-    p.keys_out[i] = keys[i];
-    p.order_out[i] = order[i];
-    const PieceAt piece = piece_at(keys, p.num_tokens, p.vocab, i);
-    if (piece.length != 0) p.pieces[atomicAdd(&counts[0], 1)] = make_int2(i, piece.length);
-    if (piece.first_of_long) p.longs[atomicAdd(&counts[1], 1)] = i;
-  }
+  for (int i = tid; i < n; i += kSmallThreads) p.order_out[base + i] = order[i];
+  for (int i0 = wave * 64; i0 < n; i0 += kSmallThreads)
+    list_pieces(
+        keys, n, ~0u, i0, base, [&](int i) { return static_cast<int32_t>(order[i]); },
+        [&](uint32_t k) { return k * kBuckets + blockIdx.x; }, counts, p.pieces + base, p.longs + base / kPiece);
   __syncthreads();
-  if (tid < 2) p.counts[tid] = counts[tid];
+  if (tid == 0) {
+    p.heads->pieces[blockIdx.x] = counts[0];
+    p.heads->longs[blockIdx.x] = counts[1];
+    p.heads->base[blockIdx.x] = base;
+  }
 }
 
 template <bool kFirst>
@@ -291,11 +382,11 @@ template <bool kFirst>
 __global__ __launch_bounds__(kTileThreads) void sort_count_kernel(SortParams p) {
   __shared__ int32_t count[kBins];
   if (static_cast<int>(blockIdx.x) >= p.zero.sorters) {
-    zero_rows<kTileThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters, reinterpret_cast<uint32_t*>(count));
+    zero_rows<kTileThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters);
     return;
   }
   const int tid = threadIdx.x;
-  if (kFirst && blockIdx.x == 0 && tid < 2) p.counts[tid] = 0;
+  if (kFirst && blockIdx.x == 0 && tid < static_cast<int>(sizeof(ListHeads) / 4)) reinterpret_cast<int32_t*>(p.heads)[tid] = 0;
   count[tid] = 0;
   __syncthreads();
   const int begin = blockIdx.x * kTile;
@@ -314,7 +405,7 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortParams p) {
   __shared__ int32_t seen[kTileWaves][kBins];
   __shared__ int32_t wave_totals[kBins / 64];
   if (static_cast<int>(blockIdx.x) >= p.zero.sorters) {
-    zero_rows<kTileThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters, reinterpret_cast<uint32_t*>(seen));
+    zero_rows<kTileThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters);
     return;
   }
   static_assert(kTileThreads == kBins, "a thread to a digit");
@@ -366,40 +457,51 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortParams p) {
   }
 }
 
-// Lists the pieces of sorted tokens.
+// Lists the pieces of sorted tokens, a wave to 64 of them; the lists follow no order (their places come
+// from counters).
 __global__ __launch_bounds__(kTileThreads) void list_pieces_kernel(SortParams p) {
-  __shared__ uint32_t marks[4096 / 32];
   if (static_cast<int>(blockIdx.x) >= p.zero.sorters) {
-    zero_rows<kTileThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters, marks);
+    zero_rows<kTileThreads>(p.zero, blockIdx.x - p.zero.sorters, gridDim.x - p.zero.sorters);
     return;
   }
-  const int i = blockIdx.x * kTileThreads + threadIdx.x;
-  if (i >= p.num_tokens) return;
-  const PieceAt piece = piece_at(p.keys_out, p.num_tokens, p.vocab, i);
-  if (piece.length != 0) p.pieces[atomicAdd(&p.counts[0], 1)] = make_int2(i, piece.length);
-  if (piece.first_of_long) p.longs[atomicAdd(&p.counts[1], 1)] = i;
+  __shared__ int32_t counts[2], places[2];
+  __shared__ Piece pieces[kTileThreads];
+  __shared__ LongRun longs[kTileThreads / kPiece + 1];
+  const int tid = threadIdx.x;
+  if (tid < 2) counts[tid] = 0;
+  __syncthreads();
+  const int i0 = blockIdx.x * kTileThreads + __builtin_amdgcn_readfirstlane(tid >> 6) * 64;
+  if (i0 < p.num_tokens)
+    list_pieces(
+        p.keys_out, p.num_tokens, p.vocab, i0, 0, [&](int i) { return p.order_out[i]; }, [](uint32_t k) { return k; },
+        counts, pieces, longs);
+  __syncthreads();
+  if (tid == 0) places[0] = atomicAdd(&p.heads->pieces[0], counts[0]);
+  if (tid == 1) places[1] = atomicAdd(&p.heads->longs[0], counts[1]);
+  __syncthreads();
+  if (tid < counts[0]) p.pieces[places[0] + tid] = pieces[tid];
+  if (tid < counts[1]) p.longs[places[1] + tid] = longs[tid];
 }
 
 // ---------------------------------------------------------------------------
 // Sums
 // ---------------------------------------------------------------------------
 struct GradParams {
-  const uint32_t* keys;   // sorted
   const int32_t* order;
   const void* dout;
   void* grad;
-  const int32_t* counts;  // pieces, runs of several
-  const int2* pieces;     // first sorted position, tokens (| kPieceOfLong)
-  const int32_t* longs;   // first sorted position
+  const ListHeads* heads;
+  const Piece* pieces;
+  const LongRun* longs;
   float* parts;           // [2 * ceil(T / kPiece)][hidden]
   int64_t dout_stride, grad_stride;
   float scale;
-  int32_t num_tokens, vocab, hidden;
+  int32_t num_tokens, hidden;
 };
 
-// Of the pieces of runs longer than one: at most one first piece, and at most one later one, starts in
-// any kPiece positions (the run between two first ones is longer, and a later piece starts that far
-// behind its predecessor), so the two places of a stretch are never shared.
+// Of the pieces of long runs at most one first and at most one later one starts in any kPiece positions
+// (the run between two first ones is longer, and a later piece starts that far behind its predecessor),
+// so the two places of a stretch are never shared.
 __device__ __forceinline__ int64_t part_of(int position, bool first) { return 2 * static_cast<int64_t>(position / kPiece) + (first ? 0 : 1); }
 
 // Eight sums to a row of the gradient, as it is typed.
@@ -424,18 +526,25 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t row, int
   }
 }
 
-// A wave to a piece and 512 columns, eight of the piece's rows in flight, added in order.
+// A wave to a piece and 512 columns, eight of the piece's rows in flight, added in order; the next piece's
+// record comes meanwhile.
 template <bool kFp32, bool kAdd>
 __global__ __launch_bounds__(256) void sum_pieces_kernel(GradParams p) {
   constexpr int kAhead = 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int blocks = (p.hidden + 511) / 512;
-  const int64_t units = static_cast<int64_t>(p.counts[0]) * blocks;
-  for (int64_t u = static_cast<int64_t>(blockIdx.x) * 4 + wave; u < units; u += static_cast<int64_t>(gridDim.x) * 4) {
-    const int2 piece = p.pieces[u / blocks];
-    const int col = static_cast<int>(u % blocks) * 512 + 8 * lane;
-    const int n = __builtin_amdgcn_readfirstlane(piece.y & (kPieceOfLong - 1));
-    const int mine = lane < n ? p.order[piece.x + lane] : 0;
+  const ListParts parts(p.heads->pieces, p.heads->base, 1);
+  const int total = parts.total();
+  PairWalk walk(blockIdx.x * 4 + wave, gridDim.x * 4, p.hidden);
+  Piece next{};
+  if (walk.entry < total) next = p.pieces[parts.at(walk.entry)];
+  while (walk.entry < total) {
+    const Piece piece = next;
+    const int col = walk.block * 512 + 8 * lane;
+    walk.go_on();
+    if (walk.entry < total) next = p.pieces[parts.at(walk.entry)];
+    const int n = __builtin_amdgcn_readfirstlane(piece.tokens & (2 * kPiece - 1));
+    int mine = piece.token;
+    if (lane > 0 && lane < n) mine = p.order[piece.at + lane];
     const bool here = col < p.hidden;
     float s[8] = {};
     for (int j0 = 0; j0 < n; j0 += kAhead) {
@@ -457,74 +566,69 @@ __global__ __launch_bounds__(256) void sum_pieces_kernel(GradParams p) {
       }
     }
     if (!here) continue;
-    const uint32_t row = p.keys[piece.x];
-    if (piece.y & kPieceOfLong) {
-      const bool first = piece.x == 0 || p.keys[piece.x - 1] != row;
-      float4* to = reinterpret_cast<float4*>(p.parts + part_of(piece.x, first) * p.hidden + col);
+    if (piece.tokens & kOfLong) {
+      float4* to = reinterpret_cast<float4*>(p.parts + part_of(piece.at, (piece.tokens & kFirst) != 0) * p.hidden + col);
       to[0] = make_float4(s[0], s[1], s[2], s[3]);
       to[1] = make_float4(s[4], s[5], s[6], s[7]);
     } else {
-      write_row<kFp32, kAdd>(p, row, col, s);
+      write_row<kFp32, kAdd>(p, piece.row, col, s);
     }
   }
 }
 
-// Adds the pieces of runs of several, in order.
+// Adds the pieces of long runs, in order.
 template <bool kFp32, bool kAdd>
 __global__ __launch_bounds__(64) void join_pieces_kernel(GradParams p) {
-  const int blocks = (p.hidden + 511) / 512;
-  const int64_t units = static_cast<int64_t>(p.counts[1]) * blocks;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int begin = p.longs[u / blocks];
-    const int col = static_cast<int>(u % blocks) * 512 + 8 * threadIdx.x;
-    const uint32_t row = p.keys[begin];
-    const int end = run_bound(p.keys, begin, p.num_tokens, row, true);
+  constexpr int kAhead = 8;
+  const ListParts parts(p.heads->longs, p.heads->base, kPiece);
+  const int total = parts.total();
+  for (PairWalk walk(blockIdx.x, gridDim.x, p.hidden); walk.entry < total; walk.go_on()) {
+    const LongRun run = p.longs[parts.at(walk.entry)];
+    const int col = walk.block * 512 + 8 * threadIdx.x;
     if (col >= p.hidden) continue;
-    constexpr int kAhead = 4;
     float s[8] = {};
-    for (int i0 = begin; i0 < end; i0 += kAhead * kPiece) {
+    for (int i0 = run.begin; i0 < run.end; i0 += kAhead * kPiece) {
       float4 q[kAhead][2];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         const int i = i0 + j * kPiece;
         q[j][0] = q[j][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i >= end) continue;
-        const float4* in = reinterpret_cast<const float4*>(p.parts + part_of(i, i == begin) * p.hidden + col);
+        if (i >= run.end) continue;
+        const float4* in = reinterpret_cast<const float4*>(p.parts + part_of(i, i == run.begin) * p.hidden + col);
         q[j][0] = in[0];
         q[j][1] = in[1];
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (i0 + j * kPiece >= end) break;
+        if (i0 + j * kPiece >= run.end) break;
         const float x[8] = {q[j][0].x, q[j][0].y, q[j][0].z, q[j][0].w, q[j][1].x, q[j][1].y, q[j][1].z, q[j][1].w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = s[e] + x[e];
       }
     }
-    write_row<kFp32, kAdd>(p, row, col, s);
+    write_row<kFp32, kAdd>(p, run.row, col, s);
   }
 }
 
 // Zeros alone, for no tokens.
 __global__ __launch_bounds__(kTileThreads) void zero_rows_kernel(ZeroParams z) {
-  __shared__ uint32_t marks[4096 / 32];
-  zero_rows<kTileThreads>(z, blockIdx.x, gridDim.x, marks);
+  zero_rows<kTileThreads>(z, blockIdx.x, gridDim.x);
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 // The workspace's parts, in order.
 struct GradSpace {
-  size_t keys, order, hist, counts, pieces, longs, parts, total;
+  size_t keys, order, hist, heads, pieces, longs, parts, total;
   GradSpace(int64_t tokens, int64_t hidden) {
     const int64_t tiles = (tokens + kTile - 1) / kTile, stretches = (tokens + kPiece - 1) / kPiece;
     keys = 0;
     order = keys + 2 * round256(4 * tokens);
     hist = order + 2 * round256(4 * tokens);
-    counts = hist + round256(4 * kBins * tiles);
-    pieces = counts + 256;
-    longs = pieces + round256(8 * tokens);
-    parts = longs + round256(4 * stretches);
+    heads = hist + round256(4 * kBins * tiles);
+    pieces = heads + round256(sizeof(ListHeads));
+    longs = pieces + round256(sizeof(Piece) * tokens);
+    parts = longs + round256(sizeof(LongRun) * stretches);
     total = parts + round256(2 * stretches * hidden * 4);
   }
 };
@@ -549,14 +653,13 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   const int size = a.grad_fp32 ? 4 : 2;
   ZeroParams z{};
   z.grad = a.grad;
-  z.ids = a.ids;
   z.row_pieces = a.grad_stride * size / 16;
   z.pieces = a.hidden_dim * size / 16;
-  z.num_tokens = a.num_tokens;
   // workgroups that write zeros beside `sorters` that sort, `threads` each: all CUs' threads
   auto zeroers = [&](int threads) {
-    const int64_t rows = z.end - z.begin, most = static_cast<int64_t>(cus) * 2048 / threads;
-    return static_cast<unsigned>(rows < most ? rows : most);
+    const int64_t waves = threads / 64, blocks = (z.end - z.begin + waves - 1) / waves;
+    const int64_t most = static_cast<int64_t>(cus) * 2048 / threads;
+    return static_cast<unsigned>(blocks < most ? blocks : most);
   };
   if (a.num_tokens == 0) {
     z.end = a.vocab;
@@ -569,20 +672,22 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   SortParams s{};
   s.ids = a.ids;
   s.hist = reinterpret_cast<int32_t*>(ws + at.hist);
-  s.counts = reinterpret_cast<int32_t*>(ws + at.counts);
-  s.pieces = reinterpret_cast<int2*>(ws + at.pieces);
-  s.longs = reinterpret_cast<int32_t*>(ws + at.longs);
+  s.heads = reinterpret_cast<ListHeads*>(ws + at.heads);
+  s.pieces = reinterpret_cast<Piece*>(ws + at.pieces);
+  s.longs = reinterpret_cast<LongRun*>(ws + at.longs);
   s.num_tokens = a.num_tokens;
   s.vocab = a.vocab;
   s.tiles = (a.num_tokens - 1) / kTile + 1;
-  int bits = 1;  // of a key, vocab the largest
-  while (bits < 31 && (a.vocab >> bits) != 0) ++bits;
+  const bool small = a.num_tokens <= kSmall;
+  const int32_t largest = small ? (a.vocab - 1) / kBuckets : a.vocab;  // of the keys
+  int bits = 1;
+  while (bits < 31 && (largest >> bits) != 0) ++bits;
   s.passes = (bits + kDigitBits - 1) / kDigitBits;
   s.bits = (bits + s.passes - 1) / s.passes;
   // the rows to clear are shared out over the launches of the sort
-  const int launches = a.num_tokens <= kSmall ? 1 : 2 * s.passes + 1;
+  const int launches = small ? 1 : 2 * s.passes + 1;
   int done = 0;
-  auto launch = [&](auto kernel, int sorters, int threads) {
+  auto launch = [&](auto kernel, int sorters, int threads, size_t lds) {
     unsigned grid = sorters;
     s.zero = z;
     s.zero.sorters = sorters;
@@ -594,7 +699,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
       grid += zeroers(threads);
     }
     ++done;
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, stream, s);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), lds, stream, s);
     return hipGetLastError();
   };
   auto buffers = [&](int side) {
@@ -604,26 +709,25 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
     s.order_out = reinterpret_cast<int32_t*>(ws + at.order + side * list);
   };
   hipError_t e = hipSuccess;
-  if (a.num_tokens <= kSmall) {
+  if (small) {
     buffers(0);
-    e = launch(sort_small_kernel, 1, kSmallThreads);
+    e = launch(sort_small_kernel, kBuckets, kSmallThreads, static_cast<size_t>(a.num_tokens) * 6);
   } else {
     for (int pass = 0; pass < s.passes && e == hipSuccess; ++pass) {
       buffers(pass & 1);
       s.shift = pass * s.bits;
-      e = pass == 0 ? launch(sort_count_kernel<true>, s.tiles, kTileThreads) : launch(sort_count_kernel<false>, s.tiles, kTileThreads);
+      e = pass == 0 ? launch(sort_count_kernel<true>, s.tiles, kTileThreads, 0) : launch(sort_count_kernel<false>, s.tiles, kTileThreads, 0);
       if (e == hipSuccess)
-        e = pass == 0 ? launch(sort_move_kernel<true>, s.tiles, kTileThreads) : launch(sort_move_kernel<false>, s.tiles, kTileThreads);
+        e = pass == 0 ? launch(sort_move_kernel<true>, s.tiles, kTileThreads, 0) : launch(sort_move_kernel<false>, s.tiles, kTileThreads, 0);
     }
-    if (e == hipSuccess) e = launch(list_pieces_kernel, (a.num_tokens - 1) / kTileThreads + 1, kTileThreads);
+    if (e == hipSuccess) e = launch(list_pieces_kernel, (a.num_tokens - 1) / kTileThreads + 1, kTileThreads, 0);
   }
   if (e != hipSuccess) return e;
   GradParams p{};
-  p.keys = s.keys_out;
   p.order = s.order_out;
   p.dout = a.dout;
   p.grad = a.grad;
-  p.counts = s.counts;
+  p.heads = s.heads;
   p.pieces = s.pieces;
   p.longs = s.longs;
   p.parts = reinterpret_cast<float*>(ws + at.parts);
@@ -631,7 +735,6 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   p.grad_stride = a.grad_stride;
   p.scale = a.scale;
   p.num_tokens = a.num_tokens;
-  p.vocab = a.vocab;
   p.hidden = a.hidden_dim;
   const int64_t units = static_cast<int64_t>(a.num_tokens) * ((a.hidden_dim + 511) / 512);
   const int64_t sum_grid = (units + 3) / 4 < 8 * cus ? (units + 3) / 4 : 8 * cus;
