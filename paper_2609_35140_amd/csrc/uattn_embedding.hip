@@ -28,6 +28,7 @@ struct EmbeddingParams {
   int64_t table_stride, out_stride;
   float scale;
   int32_t num_tokens, vocab, hidden;
+  bool stream;    // the output past the caches
   int32_t first;  // tokens of the launches before this one
 };
 
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(kEmbedWaves * 64) void embedding_kernel(EmbeddingPa
         for (int e = 0; e < 8; ++e) x[e] = x[e] * p.scale;
         w[u] = pack8(x);
       }
-      store16(p.out, to, v0 + 64 * u, w[u]);
+      store16_as(p.stream, p.out, to, v0 + 64 * u, w[u]);
     }
   }
 }
@@ -106,9 +107,7 @@ __device__ __forceinline__ uint32_t sort_key(int32_t id, int32_t vocab) {
 // The lanes of the wave whose digit is this lane's.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool valid, int bits) {
   uint64_t same = __ballot(valid);
-#pragma unroll
-  for (int b = 0; b < kDigitBits; ++b) {
-    if (b >= bits) break;
+  for (int b = 0; b < bits; ++b) {
     const uint64_t set = __ballot(digit >> b & 1);
     same &= digit >> b & 1 ? set : ~set;
   }
@@ -292,9 +291,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p)
     key[r] = p.vocab;
     if (r < rounds && begin + r * 64 < p.num_tokens) key[r] = sort_key(p.ids[begin + r * 64], p.vocab);
   }
-#pragma unroll
-  for (int r = 0; r < kSmallRounds; ++r) {
-    if (r >= rounds) break;
+  for (int r = 0; r < rounds; ++r) {
     const bool valid = key[r] < static_cast<uint32_t>(p.vocab);
     mine += __popcll(__ballot(valid && key[r] % kBuckets == blockIdx.x));
     before += __popcll(__ballot(valid && key[r] % kBuckets < blockIdx.x));
@@ -312,9 +309,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p)
     n += mine_of[w];
     base += before_of[w];
   }
-#pragma unroll
-  for (int r = 0; r < kSmallRounds; ++r) {
-    if (r >= rounds) break;
+  for (int r = 0; r < rounds; ++r) {
     const bool here = key[r] < static_cast<uint32_t>(p.vocab) && key[r] % kBuckets == blockIdx.x;
     const uint64_t all = __ballot(here);
     if (here) {
@@ -330,10 +325,8 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p)
     const uint32_t low = bins - 1;
     for (int i = tid; i < kSmallWaves * kBins; i += kSmallThreads) seen[0][i] = 0;
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSmallRounds; ++r) {
-      if (r >= rounds) break;
-      const int i = begin + r * 64;
+    for (int r = 0; r < rounds; ++r) {
+        const int i = begin + r * 64;
       key[r] = i < n ? keys[i] : 0;
       from[r] = i < n ? order[i] : 0;
       at[r] = rank_in_wave(seen[wave], key[r] >> shift & low, i < n, p.bits, lane);
@@ -349,9 +342,8 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p)
     const int32_t smaller = scan_bins(all, wave_totals);
     if (tid < kBins) first_of[tid] = smaller;
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSmallRounds; ++r) {
-      if (r >= rounds || begin + r * 64 >= n) break;
+    for (int r = 0; r < rounds; ++r) {
+      if (begin + r * 64 >= n) break;
       const uint32_t digit = key[r] >> shift & low;
       const int place = first_of[digit] + seen[wave][digit] + at[r];
       keys[place] = key[r];
@@ -636,7 +628,8 @@ struct GradSpace {
 }  // namespace
 
 hipError_t launch_embedding(const EmbeddingLaunch& a, hipStream_t stream) {
-  EmbeddingParams p{a.ids, a.table, a.out, a.table_stride, a.out_stride, a.scale, a.num_tokens, a.vocab, a.hidden_dim, 0};
+  EmbeddingParams p{a.ids, a.table, a.out, a.table_stride, a.out_stride, a.scale, a.num_tokens, a.vocab, a.hidden_dim,
+                    streams(a.num_tokens, a.hidden_dim), 0};
   return launch_parts((static_cast<int64_t>(a.num_tokens) + kEmbedWaves - 1) / kEmbedWaves, kEmbedWaves * 64,
                       [&](int first, unsigned n) {
                         p.first = first * kEmbedWaves;

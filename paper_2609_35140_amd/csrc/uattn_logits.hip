@@ -43,6 +43,7 @@ struct LogitsParams {
   const int32_t* mask_rows;  // [rows], or null: row t has mask t
   int64_t in_stride, logits_stride, out_stride, mask_stride;
   int32_t num_rows, vocab, num_tokens, num_bias, num_masks, stretches;
+  bool stream;    // the output past the caches
   int32_t rows;   // consecutive rows to a workgroup
   int32_t first;  // workgroups of the launches before this one
 };
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
       }
       const u32x4 o = pack8(x[i]);
       if (e0 + 8 <= n)
-        store16(out, 0, piece, o);
+        store16_as(p.stream, out, 0, piece, o);
       else
         for (int e = 0; e < n - e0; ++e) out[e0 + e] = static_cast<uint16_t>(o[e / 2] >> (16 * (e & 1)));
     }
@@ -310,6 +311,7 @@ hipError_t launch_logits(const LogitsLaunch& a, bool grad, hipStream_t stream) {
   p.num_bias = a.num_bias;
   p.num_masks = a.num_masks;
   p.stretches = (a.vocab - 1) / kStretch + 1;
+  p.stream = streams(a.num_rows, a.vocab);
   // few rows are spread over all CUs, many share their counts
   const int64_t share = static_cast<int64_t>(a.num_rows) * p.stretches / (16 * device_cus());
   p.rows = static_cast<int>(share < 1 ? 1 : share > kMaxRows ? kMaxRows : share);

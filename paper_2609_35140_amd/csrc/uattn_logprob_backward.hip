@@ -24,6 +24,7 @@ struct LogprobGradParams {
   const float* dlogp;
   int64_t stride, out_stride;
   int32_t vocab;
+  bool stream;  // the output past the caches
   float it, k;  // inverse temperature, and times log2(e)
   int32_t first;  // rows of the launches before this one
 };
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
   for (int i = 0; i < kVecs; ++i) {
     const int v0 = 64 * wave + i * kThreads;
     w[i] = kNegInf;
-    if (v0 < pieces && v0 + lane < pieces) w[i] = load16(x, v0 + lane);
+    if (v0 < pieces && v0 + lane < pieces) w[i] = load16(x, 0, v0 + lane);
   }
   RefSum acc{neg_infinity(), 0.f};
   // adds kN pieces, which begin at v0 + j * kThreads
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
   }
   for (int v0 = 64 * wave + kVecs * kThreads; v0 < pieces; v0 += kThreads) {
     u32x4 q = kNegInf;
-    if (v0 + lane < pieces) q = load16(x, v0 + lane);
+    if (v0 + lane < pieces) q = load16(x, 0, v0 + lane);
     add(std::integral_constant<int, 1>{}, &q, v0);
   }
   if (tail < p.vocab) {
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] = lane == at && e == (y & 7) ? at_target : t[e];
     }
-    if (v0 + lane < pieces) store16(out, v0 + lane, pack8(t));
+    if (v0 + lane < pieces) store16_as(p.stream, out, 0, v0 + lane, pack8(t));
   };
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
   }
   for (int v0 = 64 * wave + kVecs * kThreads; v0 < pieces; v0 += kThreads) {
     u32x4 q = kNegInf;
-    if (v0 + lane < pieces) q = load16(x, v0 + lane);
+    if (v0 + lane < pieces) q = load16(x, 0, v0 + lane);
     put(q, v0);
   }
   if (tail < p.vocab) {
@@ -179,6 +180,7 @@ hipError_t launch_logprob_backward(const LogprobBackwardLaunch& a, hipStream_t s
   p.stride = a.row_stride;
   p.out_stride = a.dlogits_stride;
   p.vocab = a.vocab;
+  p.stream = streams(a.num_rows, a.vocab);
   p.it = a.inv_temperature;
   p.k = static_cast<float>(static_cast<double>(a.inv_temperature) * 1.4426950408889634);
   auto launch = [&](auto threads_const, auto vecs_const) {

@@ -23,6 +23,7 @@ struct NormParams {
   int64_t gate_stride;
   float scale, eps, inv_hidden;
   int32_t num_tokens, hidden;
+  bool stream;    // the outputs past the caches
   int32_t first;  // rows of the launches before this one
 };
 
@@ -49,8 +50,8 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
   for (int i = 0; i < kVecs; ++i) {
     hw[i] = xw[i] = zero;
     if (!here || piece(i) >= pieces) continue;
-    hw[i] = load16(p.residual, base + piece(i));
-    if (p.x != nullptr) xw[i] = load16(p.x, base + piece(i));
+    hw[i] = load16(p.residual, base, piece(i));
+    if (p.x != nullptr) xw[i] = load16(p.x, base, piece(i));
   }
   float s[kVecs][8];
 #pragma unroll
@@ -74,18 +75,18 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
       float u[8], g[8];
       unpack8(xw[i], u);
       if (p.post != nullptr) {
-        unpack8(load16(p.post, piece(i)), g);
+        unpack8(load16(p.post, 0, piece(i)), g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[e] = u[e] * r * g[e];
       }
       if (p.gate != nullptr) {
-        unpack8(load16(p.gate, row * (p.gate_stride / 8) + piece(i)), g);
+        unpack8(load16(p.gate, row * (p.gate_stride / 8), piece(i)), g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[e] = u[e] * g[e];
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[i][e] = __builtin_fmaf(p.scale, u[e], s[i][e]);
-      store16(p.residual_out, base + piece(i), pack8(s[i]));
+      store16_as(p.stream, p.residual_out, base, piece(i), pack8(s[i]));
     }
   }
   if (p.y == nullptr) return;
@@ -99,10 +100,10 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
   for (int i = 0; i < kVecs; ++i) {
     if (!here || piece(i) >= pieces) break;
     float g[8];
-    unpack8(load16(p.pre, piece(i)), g);
+    unpack8(load16(p.pre, 0, piece(i)), g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) g[e] = s[i][e] * r * g[e];
-    store16(p.y, base + piece(i), pack8(g));
+    store16_as(p.stream, p.y, base, piece(i), pack8(g));
   }
 }
 
@@ -129,6 +130,7 @@ struct NormGradParams {
   int64_t gate_stride;
   float scale, eps, inv_hidden;
   int32_t num_tokens, hidden;
+  bool stream;                // the rows past the caches
   int32_t row_waves, groups;  // waves to a row, rows to a workgroup at a time
   int32_t pre_at, post_at, gate_at;  // which of the sums each is, or -1
 };
@@ -267,7 +269,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
           ds[i][e] = __builtin_fmaf(r, __builtin_fmaf(-n, dot, dy[e] * w[e]), ds[i][e]);
         }
       }
-      if (here && piece(i) < pieces) store16(p.dresidual, row * pieces, piece(i), pack8(ds[i]));
+      if (here && piece(i) < pieces) store16_as(p.stream, p.dresidual, row * pieces, piece(i), pack8(ds[i]));
     }
     if (p.dx == nullptr) continue;
     float cm = 0.f;
@@ -294,7 +296,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
         }
         if constexpr (kVecs > 1)
           if (p.gate_at >= 0) add_held(1, i, t);
-        if (p.dgate_rows != nullptr && piece(i) < pieces) store16(p.dgate_rows, row * pieces, piece(i), pack8(t));
+        if (p.dgate_rows != nullptr && piece(i) < pieces) store16_as(p.stream, p.dgate_rows, row * pieces, piece(i), pack8(t));
       }
       if (p.post != nullptr) {
         if constexpr (kVecs > 1) {
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
-      if (here && piece(i) < pieces) store16(p.dx, row * pieces, piece(i), pack8(ds[i]));
+      if (here && piece(i) < pieces) store16_as(p.stream, p.dx, row * pieces, piece(i), pack8(ds[i]));
   }
   // the row groups' column sums, in the groups' order, by the first of them
   auto put = [&](int at, const float(&d)[8], int v) {
@@ -420,7 +422,7 @@ int norm_sets(int64_t num_tokens, int64_t hidden_dim) {
 
 hipError_t launch_residual_norm(const ResidualNormLaunch& a, hipStream_t stream) {
   NormParams p{a.x, a.post_weight, a.gate, a.residual, a.pre_weight, a.residual_out, a.y, a.gate_stride, a.scale, a.eps,
-               1.0f / a.hidden_dim, a.num_tokens, a.hidden_dim, 0};
+               1.0f / a.hidden_dim, a.num_tokens, a.hidden_dim, streams(a.num_tokens, a.hidden_dim), 0};
   auto launch = [&](auto row_waves, auto vecs) {
     constexpr int kRowWaves = decltype(row_waves)::value, kVecs = decltype(vecs)::value;
     constexpr int kWaves = kNormWaves<kRowWaves>, kRows = kWaves / kRowWaves;
@@ -465,6 +467,7 @@ hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hi
   p.inv_hidden = 1.0f / a.hidden_dim;
   p.num_tokens = a.num_tokens;
   p.hidden = a.hidden_dim;
+  p.stream = streams(a.num_tokens, a.hidden_dim);
   FoldParams f{};
   f.parts = p.parts;
   f.sets = norm_sets(a.num_tokens, a.hidden_dim);

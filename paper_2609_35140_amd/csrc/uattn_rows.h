@@ -51,6 +51,24 @@ __device__ __forceinline__ void store16(void* base, int64_t uniform, uint32_t pi
   *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + 16 * uniform + 16u * piece) = w;
 }
 
+// Outputs past the caches or not.  (The empty asm keeps the two stores apart: merged, they would both be plain.)
+__device__ __forceinline__ void store16_as(bool stream, void* base, int64_t uniform, uint32_t piece, const u32x4& w) {
+  u32x4* to = reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + 16 * uniform + 16u * piece);
+  if (stream) {
+    asm volatile("" ::: "memory");
+    __builtin_nontemporal_store(w, to);
+    asm volatile("" ::: "memory");
+  } else {
+    *to = w;
+  }
+}
+// An output of bf16 rows is streamed from 64 MB on: the caches would hand little of it to the operator
+// that reads it next, and lose to it what they hold.  us for an operator and one that reads its output,
+// cached / streamed: residual norm of 4000 x 4096 (33 MB) 39 / 47, of 39,855 x 1024 (82 MB) 112 / 105, of
+// 39,855 x 4096 450 / 439; lookup of 39,855 x 4096 214 / 207 (82 MB: 46 / 48); logits of 3000 x 151,936
+// with the log-prob 529 / 500, of 300 (91 MB) 59 / 61, these with both gradients 169 / 163.
+inline bool streams(int64_t rows, int64_t width) { return 2 * rows * width >= int64_t{64} << 20; }
+
 // DPP: every lane reads another of its 16; all lanes of the patterns used have a source.
 template <int ctrl>
 __device__ __forceinline__ float dpp_read(float x) {
