@@ -7,8 +7,8 @@ PyTorch fallback -- if the library is missing, every call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Tuple
@@ -520,74 +520,64 @@ def lm_head_logprob(hidden, weight, targets, inv_temperature: float = 1.0, out=N
     return out
 
 
-# The row-wise operators below put their outputs and workspaces on the stream the
-# call runs on (torch's allocator reuses memory in a stream's order), and run on
-# their tensors' device where another one is current.
-_HERE = contextlib.nullcontext()
-
-
-def _place(device: int, stream):
+# ---------------------------------------------------------------------------
+# Row-wise operators.  Their outputs and workspaces come from the stream the call
+# runs on (torch's allocator reuses memory in a stream's order), and they run on
+# their tensors' device where another one is current: a call for another stream or
+# device repeats itself there.  A small call costs mostly Python, so a tensor is
+# checked by one expression and its message formed only where that fails.
+# ---------------------------------------------------------------------------
+def _elsewhere(device: int, stream):
+    """None where a call on `device` and `stream` runs as things are, else the context it runs in."""
     import torch
-    if stream is not None:
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=device)
-        return torch.cuda.stream(stream)
-    return _HERE if device == torch.cuda.current_device() else torch.cuda.device(device)
+    if stream is None:
+        return None if device == torch._C._cuda_getDevice() else torch.cuda.device(device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream)
 
 
-def _one_device(*tensors) -> int:
-    """The GPU that holds all the tensors (None among them is skipped)."""
-    device = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("all tensors must be on one GPU")
-    return device
+def _gpu_of(t, name) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    return t.get_device()
 
 
-def _f32_cuda(t, name):
-    import torch
-    if not (t.dtype == torch.float32 and t.is_cuda and t.is_contiguous()):
-        raise ValueError(f"{name} must be contiguous float32 on the GPU")
+def _whole(t, dtype, shape, device, name):
+    """A contiguous tensor of this type and shape on this GPU."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {device}")
 
 
-def _shaped(t, shape, name):
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be of shape {shape}")
-
-
-def _out_rows(out, rows, width, like):
-    """``out``, or new bf16 rows whose starts are 16-byte aligned."""
-    import torch
-    if out is None:
-        return torch.empty((rows, (width + 7) // 8 * 8), dtype=torch.bfloat16, device=like.device)[:, :width]
-    _bf16_rows(out, "out")
-    _shaped(out, (rows, width), "out")
-    return out
+def _rows(t, dtype, device, name):
+    """A 2-D tensor with contiguous rows, any distance apart."""
+    if t.dtype is not dtype or t.dim() != 2 or t.stride(1) != 1 or t.get_device() != device:
+        raise ValueError(f"{name} must be a 2-D {dtype} tensor with contiguous rows on GPU {device}")
 
 
 def _row_stride(t) -> int:
-    """Elements from row to row of a 2-D tensor (any would do for one row: torch may report what the call refuses)."""
+    """Elements from row to row (any would do for one row: torch may report what the call refuses)."""
     return t.stride(0) if t.shape[0] > 1 else max((t.shape[1] + 7) // 8 * 8, t.stride(0) // 8 * 8)
 
 
-def _norm_parts(residual, x, post_weight, gate, pre_weight):
-    """Checks of the residual norm's forward inputs; returns (tokens, width, gate's row stride)."""
-    _bf16_cuda(residual, "residual")
-    _need(residual.dim() == 2, "residual must be [T, H]")
-    T, H = residual.shape
-    gate_stride = 0
-    if x is not None:
-        _bf16_cuda(x, "x")
-        _shaped(x, (T, H), "x")
-    for name, w in (("post_weight", post_weight), ("pre_weight", pre_weight)):
-        if w is not None:
-            _bf16_cuda(w, name)
-            _shaped(w, (H,), name)
-    if gate is not None:
-        _bf16_cuda(gate, "gate")
-        _need(tuple(gate.shape) in ((H,), (T, H)), "gate must be [H] or [T, H]")
-        gate_stride = H if gate.dim() == 2 else 0
-    return T, H, gate_stride
+def _out_rows(out, rows, width, dtype, device):
+    """``out``, or new rows whose starts are 16-byte aligned."""
+    if out is None:
+        import torch
+        if width % 8 == 0:
+            return torch.empty((rows, width), dtype=dtype, device=device)
+        return torch.empty((rows, (width + 7) // 8 * 8), dtype=dtype, device=device)[:, :width]
+    _rows(out, dtype, device, "out")
+    _need(out.shape == (rows, width), "out shape")
+    return out
+
+
+def _workspace(workspace, need: int, device):
+    if workspace is None:
+        import torch
+        return torch.empty(need if need > 16 else 16, dtype=torch.uint8, device=device)  # no initial contents needed
+    _need(workspace.get_device() == device and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
+    return workspace
 
 
 def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6,
@@ -602,35 +592,46 @@ def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None
       is no pre_weight.  residual_out may be residual, y may be x (in place).
     """
     import torch
-    T, H, gate_stride = _norm_parts(residual, x, post_weight, gate, pre_weight)
-    _need(x is not None or pre_weight is not None, "x or pre_weight must be given")
-    _need(x is not None or (post_weight is None and gate is None and residual_out is None),
-          "post_weight, gate and residual_out belong to x")
-    _need(pre_weight is not None or y is None, "y belongs to pre_weight")
-    for name, t in (("residual_out", residual_out), ("y", y)):
-        if t is not None:
-            _bf16_cuda(t, name)
-            _shaped(t, (T, H), name)
-    with _place(_one_device(residual, x, post_weight, gate, pre_weight, residual_out, y), stream):
-        if x is not None and residual_out is None:
+    dev = _gpu_of(residual, "residual")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return residual_norm(residual, pre_weight, x, post_weight, gate, scale, eps, residual_out, y)
+    bf16, shape = torch.bfloat16, residual.shape
+    _need(len(shape) == 2, "residual must be [T, H]")
+    T, H = shape
+    _whole(residual, bf16, shape, dev, "residual")
+    gate_stride = 0
+    if x is None:
+        _need(pre_weight is not None, "x or pre_weight must be given")
+        _need(post_weight is None and gate is None and residual_out is None, "post_weight, gate and residual_out belong to x")
+    else:
+        _whole(x, bf16, shape, dev, "x")
+        if post_weight is not None:
+            _whole(post_weight, bf16, (H,), dev, "post_weight")
+        if gate is not None:
+            gate_stride = H if gate.dim() == 2 else 0
+            _whole(gate, bf16, shape if gate_stride else (H,), dev, "gate")
+        if residual_out is None:
             residual_out = torch.empty_like(residual)
-        if pre_weight is not None and y is None:
+        else:
+            _whole(residual_out, bf16, shape, dev, "residual_out")
+    if pre_weight is None:
+        _need(y is None, "y belongs to pre_weight")
+    else:
+        _whole(pre_weight, bf16, (H,), dev, "pre_weight")
+        if y is None:
             y = torch.empty_like(residual)
-        _check(_load().uattn_residual_norm(_ptr(x), _ptr(post_weight), _ptr(gate), gate_stride, scale, _ptr(residual),
-                                           _ptr(pre_weight), eps, T, H, _ptr(residual_out), _ptr(y), _stream(None)))
+        else:
+            _whole(y, bf16, shape, dev, "y")
+    _check(_load().uattn_residual_norm(_ptr(x), _ptr(post_weight), _ptr(gate), gate_stride, scale, residual.data_ptr(),
+                                       _ptr(pre_weight), eps, T, H, _ptr(residual_out), _ptr(y), _stream(None)))
     return (residual if x is None else residual_out), y
 
 
+@functools.lru_cache(maxsize=256)
 def residual_norm_backward_workspace_bytes(num_tokens: int, hidden_dim: int) -> int:
     return int(_load().uattn_residual_norm_backward_workspace_bytes(int(num_tokens), int(hidden_dim)))
-
-
-def _workspace(workspace, need: int, device):
-    import torch
-    if workspace is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)  # no initial contents needed
-    _need(workspace.is_cuda and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
-    return workspace
 
 
 def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=None, post_weight=None, gate=None,
@@ -648,7 +649,16 @@ def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=N
       what the forward did not have.
     """
     import torch
-    T, H, gate_stride = _norm_parts(residual_out, x, post_weight, gate, pre_weight)
+    dev = _gpu_of(residual_out, "residual_out")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return residual_norm_backward(dy, dresidual_out, residual_out, pre_weight, x, post_weight, gate, scale, eps,
+                                          dresidual, dx, has_block, workspace)
+    bf16, shape = torch.bfloat16, residual_out.shape
+    _need(len(shape) == 2, "residual_out must be [T, H]")
+    T, H = shape
+    _whole(residual_out, bf16, shape, dev, "residual_out")
     if has_block is None:
         has_block = x is not None
     _need(has_block or (post_weight is None and gate is None and x is None and dx is None),
@@ -656,29 +666,37 @@ def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=N
     _need(x is not None or (post_weight is None and gate is None), "the gradients of post_weight and gate need x")
     _need((dy is None) == (pre_weight is None), "dy and pre_weight belong together")
     _need(dy is not None or dresidual_out is not None, "dy or dresidual_out must be given")
-    for name, t in (("dy", dy), ("dresidual_out", dresidual_out), ("dresidual", dresidual), ("dx", dx)):
+    for name, t in (("dy", dy), ("dresidual_out", dresidual_out), ("x", x), ("dresidual", dresidual), ("dx", dx)):
         if t is not None:
-            _bf16_cuda(t, name)
-            _shaped(t, (T, H), name)
-    dpre = dpost = dgate = None
-    device = residual_out.device
-    with _place(_one_device(residual_out, dy, dresidual_out, x, post_weight, gate, pre_weight, dresidual, dx, workspace), stream):
-        if dresidual is None:
-            dresidual = torch.empty_like(residual_out)
-        if has_block and dx is None:
-            dx = torch.empty_like(residual_out)
-        if pre_weight is not None:
-            dpre = torch.empty(H, dtype=torch.float32, device=device)
-        if post_weight is not None:
-            dpost = torch.empty(H, dtype=torch.float32, device=device)
-        if gate is not None:
-            dgate = torch.empty_like(gate) if gate_stride else torch.empty(H, dtype=torch.float32, device=device)
-        workspace = _workspace(workspace, residual_norm_backward_workspace_bytes(T, H), device)
-        _check(_load().uattn_residual_norm_backward(
-            _ptr(dy), _ptr(dresidual_out), _ptr(residual_out), _ptr(pre_weight), _ptr(x), _ptr(post_weight), _ptr(gate),
-            gate_stride, scale, eps, T, H, _ptr(dresidual), _ptr(dx), _ptr(dpre), _ptr(dpost), _ptr(dgate),
-            _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(None)))
-    return dresidual, dx, dpre, dpost, dgate
+            _whole(t, bf16, shape, dev, name)
+    gate_stride = 0
+    if gate is not None:
+        gate_stride = H if gate.dim() == 2 else 0
+        _whole(gate, bf16, shape if gate_stride else (H,), dev, "gate")
+    sums = []
+    if pre_weight is not None:
+        _whole(pre_weight, bf16, (H,), dev, "pre_weight")
+        sums.append(0)
+    if post_weight is not None:
+        _whole(post_weight, bf16, (H,), dev, "post_weight")
+        sums.append(1)
+    if gate is not None and not gate_stride:
+        sums.append(2)
+    if dresidual is None:
+        dresidual = torch.empty_like(residual_out)
+    if has_block and dx is None:
+        dx = torch.empty_like(residual_out)
+    d = [None, None, torch.empty_like(gate) if gate_stride else None]
+    if sums:
+        # one allocation; every row starts 16-byte aligned, as H is a multiple of 8 in calls that are not refused
+        for i, row in zip(sums, torch.empty((len(sums), H), dtype=torch.float32, device=dev).unbind(0)):
+            d[i] = row
+    workspace = _workspace(workspace, residual_norm_backward_workspace_bytes(T, H), dev)
+    _check(_load().uattn_residual_norm_backward(
+        _ptr(dy), _ptr(dresidual_out), residual_out.data_ptr(), _ptr(pre_weight), _ptr(x), _ptr(post_weight), _ptr(gate),
+        gate_stride, scale, eps, T, H, dresidual.data_ptr(), _ptr(dx), _ptr(d[0]), _ptr(d[1]), _ptr(d[2]),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(None)))
+    return dresidual, dx, d[0], d[1], d[2]
 
 
 def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
@@ -686,17 +704,23 @@ def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
 
       ids [T] int32 (negative: padding, a row of zeros); table [V, H] bf16 (rows may be strided); returns [T, H] bf16.
     """
-    _i32_cuda(ids, "ids")
-    _bf16_rows(table, "table")
+    import torch
+    dev = _gpu_of(table, "table")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return embedding(ids, table, scale, out)
+    _rows(table, torch.bfloat16, dev, "table")
     _need(ids.dim() == 1, "ids must be [T]")
+    _whole(ids, torch.int32, ids.shape, dev, "ids")
     T, (V, H) = ids.shape[0], table.shape
-    with _place(_one_device(ids, table, out), stream):
-        out = _out_rows(out, T, H, table)
-        _check(_load().uattn_embedding(_ptr(ids), _ptr(table), _row_stride(table), scale, T, V, H, _ptr(out),
-                                       _row_stride(out), _stream(None)))
+    out = _out_rows(out, T, H, torch.bfloat16, dev)
+    _check(_load().uattn_embedding(ids.data_ptr(), table.data_ptr(), _row_stride(table), scale, T, V, H, out.data_ptr(),
+                                   _row_stride(out), _stream(None)))
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def embedding_backward_workspace_bytes(num_tokens: int, hidden_dim: int) -> int:
     return int(_load().uattn_embedding_backward_workspace_bytes(int(num_tokens), int(hidden_dim)))
 
@@ -711,10 +735,14 @@ def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, acc
       are; without, those rows become zeros.
     """
     import torch
-    _bf16_rows(dout, "dout")
-    _i32_cuda(ids, "ids")
+    dev = _gpu_of(dout, "dout")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return embedding_backward(dout, ids, vocab, scale, grad, accumulate, dtype, workspace)
+    _rows(dout, torch.bfloat16, dev, "dout")
     T, H = dout.shape
-    _need(ids.shape == (T,), "ids must be [T]")
+    _whole(ids, torch.int32, (T,), dev, "ids")
     vocab = int(vocab)
     if grad is None:
         _need(not accumulate, "accumulate needs grad")
@@ -722,49 +750,48 @@ def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, acc
     else:
         _need(dtype is None or dtype == grad.dtype, "grad is of another dtype")
         dtype = grad.dtype
-        _need(grad.is_cuda and grad.dim() == 2 and grad.stride(1) == 1, "grad must be a 2-D GPU tensor with contiguous rows")
-        _shaped(grad, (vocab, H), "grad")
+        _rows(grad, dtype, dev, "grad")
+        _need(grad.shape == (vocab, H), "grad must be [vocab, H]")
     _need(dtype in (torch.float32, torch.bfloat16), "grad must be float32 or bfloat16")
-    with _place(_one_device(dout, ids, grad, workspace), stream):
-        if grad is None:
-            grad = torch.empty((vocab, H), dtype=dtype, device=dout.device)
-        workspace = _workspace(workspace, embedding_backward_workspace_bytes(T, H), dout.device)
-        _check(_load().uattn_embedding_backward(
-            _ptr(dout), _row_stride(dout), _ptr(ids), scale, T, vocab, H, _ptr(grad), _row_stride(grad),
-            int(dtype == torch.float32), int(bool(accumulate)), _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream(None)))
+    if grad is None:
+        _need(vocab >= 0, "vocab must not be negative")
+        grad = torch.empty((vocab, H), dtype=dtype, device=dev)
+    workspace = _workspace(workspace, embedding_backward_workspace_bytes(T, H), dev)
+    _check(_load().uattn_embedding_backward(
+        dout.data_ptr(), _row_stride(dout), ids.data_ptr(), scale, T, vocab, H, grad.data_ptr(), _row_stride(grad),
+        int(dtype == torch.float32), int(bool(accumulate)), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(None)))
     return grad
 
 
-def _penalty_parts(rows, tokens, history, penalties):
-    _need((history is None) == (penalties is None) and (history is None) == (tokens is None),
-          "tokens, history and penalties belong together")
+def _penalty_parts(rows, tokens, history, penalties, dev) -> int:
+    """Checks; how many tokens there are."""
     if history is None:
+        _need(tokens is None and penalties is None, "tokens, history and penalties belong together")
         return 0
-    _i32_cuda(tokens, "tokens")
-    _i32_cuda(history, "history")
-    _f32_cuda(penalties, "penalties")
+    import torch
+    _need(tokens is not None and penalties is not None, "tokens, history and penalties belong together")
     _need(tokens.dim() == 1, "tokens must be 1-D")
-    _shaped(history, (rows, 3), "history")
-    _shaped(penalties, (rows, 3), "penalties")
+    _whole(tokens, torch.int32, tokens.shape, dev, "tokens")
+    _whole(history, torch.int32, (rows, 3), dev, "history")
+    _whole(penalties, torch.float32, (rows, 3), dev, "penalties")
     return tokens.shape[0]
 
 
-def _mask_parts(rows, vocab, mask, mask_rows):
-    """(masks, words from mask to mask)"""
-    _need(mask is not None or mask_rows is None, "mask_rows belongs to mask")
+def _mask_parts(rows, vocab, mask, mask_rows, dev) -> Tuple[int, int]:
+    """Checks; (masks, words from mask to mask)"""
     if mask is None:
+        _need(mask_rows is None, "mask_rows belongs to mask")
         return 0, 0
     import torch
-    _need(mask.is_cuda and mask.dtype == torch.int32 and mask.dim() == 2 and mask.stride(1) == 1,
-          "mask must be a 2-D int32 GPU tensor with contiguous rows")
-    _need(mask.shape[1] >= (vocab + 31) // 32, "mask must have a bit for every vocabulary entry")
+    _rows(mask, torch.int32, dev, "mask")
+    masks, words = mask.shape
+    _need(words >= (vocab + 31) // 32, "mask must have a bit for every vocabulary entry")
     if mask_rows is None:
-        _need(mask.shape[0] >= rows, "mask needs a row for every row of logits, or mask_rows")
+        _need(masks >= rows, "mask needs a row for every row of logits, or mask_rows")
     else:
-        _i32_cuda(mask_rows, "mask_rows")
-        _shaped(mask_rows, (rows,), "mask_rows")
-    return mask.shape[0], mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
+        _whole(mask_rows, torch.int32, (rows,), dev, "mask_rows")
+    return masks, mask.stride(0) if masks > 1 else words
 
 
 def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=None, bias_values=None, bias_rows=None,
@@ -778,26 +805,31 @@ def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=N
       int32 words (a set bit allows), mask_rows [T] int32 (negative: no mask).
       Returns bf16 [T, V]; out may be logits (in place).
     """
-    _bf16_rows(logits, "logits")
+    import torch
+    dev = _gpu_of(logits, "logits")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return logits_process(logits, tokens, history, penalties, bias_ids, bias_values, bias_rows, mask, mask_rows, out)
+    _rows(logits, torch.bfloat16, dev, "logits")
     T, V = logits.shape
-    num_tokens = _penalty_parts(T, tokens, history, penalties)
-    num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows)
+    num_tokens = _penalty_parts(T, tokens, history, penalties, dev)
+    num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows, dev)
     num_bias = 0
-    _need((bias_rows is None) == (bias_ids is None) and (bias_rows is None) == (bias_values is None),
-          "bias_ids, bias_values and bias_rows belong together")
-    if bias_rows is not None:
-        _i32_cuda(bias_ids, "bias_ids")
-        _f32_cuda(bias_values, "bias_values")
-        _i32_cuda(bias_rows, "bias_rows")
-        _need(bias_ids.dim() == 1 and bias_values.shape == bias_ids.shape, "bias_ids and bias_values must be [M]")
-        _shaped(bias_rows, (T, 2), "bias_rows")
+    if bias_rows is None:
+        _need(bias_ids is None and bias_values is None, "bias_ids, bias_values and bias_rows belong together")
+    else:
+        _need(bias_ids is not None and bias_values is not None, "bias_ids, bias_values and bias_rows belong together")
+        _need(bias_ids.dim() == 1, "bias_ids must be [M]")
+        _whole(bias_ids, torch.int32, bias_ids.shape, dev, "bias_ids")
+        _whole(bias_values, torch.float32, bias_ids.shape, dev, "bias_values")
+        _whole(bias_rows, torch.int32, (T, 2), dev, "bias_rows")
         num_bias = bias_ids.shape[0]
-    with _place(_one_device(logits, tokens, history, penalties, bias_ids, bias_values, bias_rows, mask, mask_rows, out), stream):
-        out = _out_rows(out, T, V, logits)
-        _check(_load().uattn_logits_process(
-            _ptr(logits), _row_stride(logits), T, V, _ptr(tokens), num_tokens, _ptr(history), _ptr(penalties),
-            _ptr(bias_ids), _ptr(bias_values), num_bias, _ptr(bias_rows), _ptr(mask), mask_stride, num_masks,
-            _ptr(mask_rows), _ptr(out), _row_stride(out), _stream(None)))
+    out = _out_rows(out, T, V, torch.bfloat16, dev)
+    _check(_load().uattn_logits_process(
+        logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens, _ptr(history), _ptr(penalties),
+        _ptr(bias_ids), _ptr(bias_values), num_bias, _ptr(bias_rows), _ptr(mask), mask_stride, num_masks,
+        _ptr(mask_rows), out.data_ptr(), _row_stride(out), _stream(None)))
     return out
 
 
@@ -808,18 +840,23 @@ def logits_process_backward(dout, logits, tokens=None, history=None, penalties=N
       dout [T, V] bf16, gradient of the processed logits; the others as passed to
       logits_process.  Returns bf16 [T, V]; out may be dout (in place).
     """
-    _bf16_rows(dout, "dout")
-    _bf16_rows(logits, "logits")
+    import torch
+    dev = _gpu_of(logits, "logits")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return logits_process_backward(dout, logits, tokens, history, penalties, mask, mask_rows, out)
+    _rows(logits, torch.bfloat16, dev, "logits")
+    _rows(dout, torch.bfloat16, dev, "dout")
     T, V = logits.shape
-    _shaped(dout, (T, V), "dout")
-    num_tokens = _penalty_parts(T, tokens, history, penalties)
-    num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows)
-    with _place(_one_device(dout, logits, tokens, history, penalties, mask, mask_rows, out), stream):
-        out = _out_rows(out, T, V, logits)
-        _check(_load().uattn_logits_process_backward(
-            _ptr(dout), _row_stride(dout), _ptr(logits), _row_stride(logits), T, V, _ptr(tokens), num_tokens,
-            _ptr(history), _ptr(penalties), _ptr(mask), mask_stride, num_masks, _ptr(mask_rows), _ptr(out),
-            _row_stride(out), _stream(None)))
+    _need(dout.shape == (T, V), "dout must be of the logits' shape")
+    num_tokens = _penalty_parts(T, tokens, history, penalties, dev)
+    num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows, dev)
+    out = _out_rows(out, T, V, torch.bfloat16, dev)
+    _check(_load().uattn_logits_process_backward(
+        dout.data_ptr(), _row_stride(dout), logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens,
+        _ptr(history), _ptr(penalties), _ptr(mask), mask_stride, num_masks, _ptr(mask_rows), out.data_ptr(),
+        _row_stride(out), _stream(None)))
     return out
 
 
@@ -829,16 +866,19 @@ def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=N
       logits [T, V] bf16 and targets [T] int32 as passed to logprob; dlogp [T] fp32
       (0: the row gets zeros).  Returns bf16 [T, V].
     """
-    _bf16_rows(logits, "logits")
+    import torch
+    dev = _gpu_of(logits, "logits")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return logprob_backward(logits, targets, dlogp, inv_temperature, out)
+    _rows(logits, torch.bfloat16, dev, "logits")
     T, V = logits.shape
-    _i32_cuda(targets, "targets")
-    _f32_cuda(dlogp, "dlogp")
-    _shaped(targets, (T,), "targets")
-    _shaped(dlogp, (T,), "dlogp")
-    with _place(_one_device(logits, targets, dlogp, out), stream):
-        out = _out_rows(out, T, V, logits)
-        _check(_load().uattn_logprob_backward(_ptr(logits), _row_stride(logits), _ptr(targets), _ptr(dlogp), T, V,
-                                              inv_temperature, _ptr(out), _row_stride(out), _stream(None)))
+    _whole(targets, torch.int32, (T,), dev, "targets")
+    _whole(dlogp, torch.float32, (T,), dev, "dlogp")
+    out = _out_rows(out, T, V, torch.bfloat16, dev)
+    _check(_load().uattn_logprob_backward(logits.data_ptr(), _row_stride(logits), targets.data_ptr(), dlogp.data_ptr(), T, V,
+                                          inv_temperature, out.data_ptr(), _row_stride(out), _stream(None)))
     return out
 
 
