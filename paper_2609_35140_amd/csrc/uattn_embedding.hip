@@ -519,9 +519,10 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t row, int
 }
 
 // A wave to a piece and 512 columns, eight of the piece's rows in flight, added in order; the next piece's
-// record comes meanwhile.
+// record comes meanwhile.  Pieces differ in length, so a CU gets 32 workgroups one after another, not all
+// of its work at once (16,384 tokens, 32,000 x 4096 bf16: 116 us with 8 to a CU, 110 with 32, 113 with 128).
 template <bool kFp32, bool kAdd>
-__global__ __launch_bounds__(256) void sum_pieces_kernel(GradParams p) {
+__global__ __launch_bounds__(256, 6) void sum_pieces_kernel(GradParams p) {
   constexpr int kAhead = 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const ListParts parts(p.heads->pieces, p.heads->base, 1);
@@ -571,7 +572,7 @@ __global__ __launch_bounds__(256) void sum_pieces_kernel(GradParams p) {
 // Adds the pieces of long runs, in order.
 template <bool kFp32, bool kAdd>
 __global__ __launch_bounds__(64) void join_pieces_kernel(GradParams p) {
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 16;
   const ListParts parts(p.heads->longs, p.heads->base, kPiece);
   const int total = parts.total();
   for (PairWalk walk(blockIdx.x, gridDim.x, p.hidden); walk.entry < total; walk.go_on()) {
@@ -730,7 +731,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   p.num_tokens = a.num_tokens;
   p.hidden = a.hidden_dim;
   const int64_t units = static_cast<int64_t>(a.num_tokens) * ((a.hidden_dim + 511) / 512);
-  const int64_t sum_grid = (units + 3) / 4 < 8 * cus ? (units + 3) / 4 : 8 * cus;
+  const int64_t sum_grid = (units + 3) / 4 < 32 * cus ? (units + 3) / 4 : 32 * cus;
   const int64_t join_grid = units / kPiece + 1 < 16 * cus ? units / kPiece + 1 : 16 * cus;
   auto sums = [&](auto fp32, auto add) {
     constexpr bool kFp32 = decltype(fp32)::value, kAdd = decltype(add)::value;
