@@ -46,9 +46,9 @@ __device__ __forceinline__ RefSum combine(RefSum a, RefSum b) {
 // What is subtracted from the exponents: a reference of -inf (nothing but masked entries) subtracts nothing.
 __device__ __forceinline__ float shift_of(float ref) { return ref == neg_infinity() ? 0.f : ref; }
 
-// The row stays in registers between its sum and its gradient (kVecs 16-byte pieces to a thread, all
-// requested at once): it is read from memory once and written once.  Pieces past kThreads * kVecs are
-// read again.
+// Bound by memory.  The row stays in registers between its sum and its gradient (kVecs 16-byte pieces to
+// a thread, all requested at once): it is read once and written once (4100 rows of 151,936: 481 us, 5.2 TB/s;
+// read a second time from the caches it took 1755).  Pieces past kThreads * kVecs are read again.
 template <int kThreads, int kVecs>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParams p) {
   constexpr int kWaves = kThreads / 64;
@@ -190,10 +190,14 @@ hipError_t launch_logprob_backward(const LogprobBackwardLaunch& a, hipStream_t s
       hipLaunchKernelGGL((logprob_grad_kernel<kThreads, kVecs>), dim3(n), dim3(kThreads), 0, stream, p);
     });
   };
+  // Threads and pieces by the vocabulary alone (a row's bits do not depend on the number of rows): four to
+  // nineteen pieces in flight to a thread, and two rows or more to a CU up to 65,536 entries, so that one is
+  // read while the other is written.  us for 600 and for 3000 rows: 32,000 entries 512 x 8 17.5 / 71, 256 x 16
+  // 18.9 / 73.5; 50,257 512 x 16 28 / 116, 1024 x 8 35 / 136; 8000 128 x 8 8.6 / 17.6, 256 x 4 8.9 / 18.7.
   using std::integral_constant;
   if (a.vocab <= 2048) return launch(integral_constant<int, 64>{}, integral_constant<int, 4>{});
   if (a.vocab <= 8192) return launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
-  if (a.vocab <= 32768) return launch(integral_constant<int, 256>{}, integral_constant<int, 16>{});
+  if (a.vocab <= 32768) return launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
   if (a.vocab <= 65536) return launch(integral_constant<int, 512>{}, integral_constant<int, 16>{});
   if (a.vocab <= 131072) return launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
   return launch(integral_constant<int, 1024>{}, integral_constant<int, 19>{});

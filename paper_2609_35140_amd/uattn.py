@@ -560,23 +560,22 @@ def _row_stride(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else max((t.shape[1] + 7) // 8 * 8, t.stride(0) // 8 * 8)
 
 
-def _out_rows(out, rows, width, dtype, device):
-    """``out``, or new rows whose starts are 16-byte aligned."""
+def _out_rows(out, like, rows, width):
+    """``out``, or new rows of ``like``'s type and device whose starts are 16-byte aligned."""
     if out is None:
-        import torch
         if width % 8 == 0:
-            return torch.empty((rows, width), dtype=dtype, device=device)
-        return torch.empty((rows, (width + 7) // 8 * 8), dtype=dtype, device=device)[:, :width]
-    _rows(out, dtype, device, "out")
+            return like.new_empty((rows, width))
+        return like.new_empty((rows, (width + 7) // 8 * 8))[:, :width]
+    _rows(out, like.dtype, like.get_device(), "out")
     _need(out.shape == (rows, width), "out shape")
     return out
 
 
-def _workspace(workspace, need: int, device):
+def _workspace(workspace, need: int, like):
     if workspace is None:
         import torch
-        return torch.empty(need if need > 16 else 16, dtype=torch.uint8, device=device)  # no initial contents needed
-    _need(workspace.get_device() == device and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
+        return like.new_empty(need if need > 16 else 16, dtype=torch.uint8)  # no initial contents needed
+    _need(workspace.get_device() == like.get_device() and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
     return workspace
 
 
@@ -687,11 +686,13 @@ def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=N
     if has_block and dx is None:
         dx = torch.empty_like(residual_out)
     d = [None, None, torch.empty_like(gate) if gate_stride else None]
-    if sums:
+    if len(sums) == 1:
+        d[sums[0]] = residual_out.new_empty(H, dtype=torch.float32)
+    elif sums:
         # one allocation; every row starts 16-byte aligned, as H is a multiple of 8 in calls that are not refused
-        for i, row in zip(sums, torch.empty((len(sums), H), dtype=torch.float32, device=dev).unbind(0)):
+        for i, row in zip(sums, residual_out.new_empty((len(sums), H), dtype=torch.float32).unbind(0)):
             d[i] = row
-    workspace = _workspace(workspace, residual_norm_backward_workspace_bytes(T, H), dev)
+    workspace = _workspace(workspace, residual_norm_backward_workspace_bytes(T, H), residual_out)
     _check(_load().uattn_residual_norm_backward(
         _ptr(dy), _ptr(dresidual_out), residual_out.data_ptr(), _ptr(pre_weight), _ptr(x), _ptr(post_weight), _ptr(gate),
         gate_stride, scale, eps, T, H, dresidual.data_ptr(), _ptr(dx), _ptr(d[0]), _ptr(d[1]), _ptr(d[2]),
@@ -714,7 +715,7 @@ def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
     _need(ids.dim() == 1, "ids must be [T]")
     _whole(ids, torch.int32, ids.shape, dev, "ids")
     T, (V, H) = ids.shape[0], table.shape
-    out = _out_rows(out, T, H, torch.bfloat16, dev)
+    out = _out_rows(out, table, T, H)
     _check(_load().uattn_embedding(ids.data_ptr(), table.data_ptr(), _row_stride(table), scale, T, V, H, out.data_ptr(),
                                    _row_stride(out), _stream(None)))
     return out
@@ -755,8 +756,8 @@ def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, acc
     _need(dtype in (torch.float32, torch.bfloat16), "grad must be float32 or bfloat16")
     if grad is None:
         _need(vocab >= 0, "vocab must not be negative")
-        grad = torch.empty((vocab, H), dtype=dtype, device=dev)
-    workspace = _workspace(workspace, embedding_backward_workspace_bytes(T, H), dev)
+        grad = dout.new_empty((vocab, H), dtype=dtype)
+    workspace = _workspace(workspace, embedding_backward_workspace_bytes(T, H), dout)
     _check(_load().uattn_embedding_backward(
         dout.data_ptr(), _row_stride(dout), ids.data_ptr(), scale, T, vocab, H, grad.data_ptr(), _row_stride(grad),
         int(dtype == torch.float32), int(bool(accumulate)), workspace.data_ptr(),
@@ -825,7 +826,7 @@ def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=N
         _whole(bias_values, torch.float32, bias_ids.shape, dev, "bias_values")
         _whole(bias_rows, torch.int32, (T, 2), dev, "bias_rows")
         num_bias = bias_ids.shape[0]
-    out = _out_rows(out, T, V, torch.bfloat16, dev)
+    out = _out_rows(out, logits, T, V)
     _check(_load().uattn_logits_process(
         logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens, _ptr(history), _ptr(penalties),
         _ptr(bias_ids), _ptr(bias_values), num_bias, _ptr(bias_rows), _ptr(mask), mask_stride, num_masks,
@@ -852,7 +853,7 @@ def logits_process_backward(dout, logits, tokens=None, history=None, penalties=N
     _need(dout.shape == (T, V), "dout must be of the logits' shape")
     num_tokens = _penalty_parts(T, tokens, history, penalties, dev)
     num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows, dev)
-    out = _out_rows(out, T, V, torch.bfloat16, dev)
+    out = _out_rows(out, logits, T, V)
     _check(_load().uattn_logits_process_backward(
         dout.data_ptr(), _row_stride(dout), logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens,
         _ptr(history), _ptr(penalties), _ptr(mask), mask_stride, num_masks, _ptr(mask_rows), out.data_ptr(),
@@ -876,7 +877,7 @@ def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=N
     T, V = logits.shape
     _whole(targets, torch.int32, (T,), dev, "targets")
     _whole(dlogp, torch.float32, (T,), dev, "dlogp")
-    out = _out_rows(out, T, V, torch.bfloat16, dev)
+    out = _out_rows(out, logits, T, V)
     _check(_load().uattn_logprob_backward(logits.data_ptr(), _row_stride(logits), targets.data_ptr(), dlogp.data_ptr(), T, V,
                                           inv_temperature, out.data_ptr(), _row_stride(out), _stream(None)))
     return out
