@@ -489,8 +489,9 @@ size_t uattn_embedding_backward_workspace_bytes(int32_t num_tokens, int32_t hidd
  *   8; dout_stride a multiple of 8, grad_stride of 16 bytes; pointers 16-byte aligned.
  *
  * The tokens are sorted by id; an entry's rows are added in ascending order of t
- * in fp32, 32 at a time, then these sums in order, with one rounding at the end:
- * a row's bits depend on its own tokens alone, and repeated calls give the same.
+ * in fp32, 32 at a time, then these sums (in eight equal parts, each in order),
+ * with one rounding at the end: a row's bits depend on its own tokens alone, and
+ * repeated calls give the same.
  */
 uattn_status uattn_embedding_backward(const void* dout, int64_t dout_stride, const int32_t* ids, float scale,
                                       int32_t num_tokens, int32_t vocab, int32_t hidden_dim, void* grad,

@@ -258,7 +258,7 @@ struct SortParams {
   const int32_t* order_in;
   uint32_t* keys_out;
   int32_t* order_out;
-  int32_t* hist;                 // [tiles][kBins]
+  int32_t* hist;                 // [tiles + 1][kBins]; of many tiles, summed: before the tile, and of all behind the last
   ListHeads* heads;
   Piece* pieces;
   LongRun* longs;
@@ -391,6 +391,28 @@ __global__ __launch_bounds__(kTileThreads) void sort_count_kernel(SortParams p) 
   p.hist[static_cast<int64_t>(blockIdx.x) * kBins + tid] = count[tid];
 }
 
+// Up to kManyTiles every workgroup sums the digits' counts of all tiles for itself; past them, where that
+// grows with the square of the tiles, a launch does it for all: each digit's counts become those of the tiles
+// before.  (256 tiles of 2048 tokens: a pass takes 30 us so, and 18 + 12 with the launch.)
+constexpr int kManyTiles = 256;
+
+__global__ __launch_bounds__(64) void sum_tiles_kernel(int32_t* hist, int32_t tiles) {
+  int32_t* at = hist + blockIdx.x * 64 + threadIdx.x;
+  constexpr int kAhead = 16;
+  int32_t sum = 0;
+  for (int32_t t0 = 0; t0 < tiles; t0 += kAhead) {
+    int32_t n[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) n[u] = t0 + u < tiles ? at[static_cast<int64_t>(t0 + u) * kBins] : 0;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (t0 + u < tiles) at[static_cast<int64_t>(t0 + u) * kBins] = sum;
+      sum += n[u];
+    }
+  }
+  at[static_cast<int64_t>(tiles) * kBins] = sum;
+}
+
 // Moves a tile's tokens behind the smaller digits of all tiles and the equal ones of the tiles before.
 template <bool kFirst>
 __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortParams p) {
@@ -418,15 +440,20 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortParams p) {
   for (int w = 0; w < kTileWaves; ++w) seen[w][tid] = 0;
   // of this thread's digit: all its tokens, and those in the tiles before this one
   int32_t all = 0, earlier = 0;
-  constexpr int kAhead = 8;
-  for (int t0 = 0; t0 < p.tiles; t0 += kAhead) {
-    int32_t n[kAhead];
+  if (p.tiles > kManyTiles) {
+    earlier = p.hist[static_cast<int64_t>(blockIdx.x) * kBins + tid];
+    all = p.hist[static_cast<int64_t>(p.tiles) * kBins + tid];
+  } else {
+    constexpr int kAhead = 8;
+    for (int t0 = 0; t0 < p.tiles; t0 += kAhead) {
+      int32_t n[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) n[u] = t0 + u < p.tiles ? p.hist[static_cast<int64_t>(t0 + u) * kBins + tid] : 0;
+      for (int u = 0; u < kAhead; ++u) n[u] = t0 + u < p.tiles ? p.hist[static_cast<int64_t>(t0 + u) * kBins + tid] : 0;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      all += n[u];
-      if (t0 + u < static_cast<int>(blockIdx.x)) earlier += n[u];
+      for (int u = 0; u < kAhead; ++u) {
+        all += n[u];
+        if (t0 + u < static_cast<int>(blockIdx.x)) earlier += n[u];
+      }
     }
   }
   __syncthreads();
@@ -569,37 +596,51 @@ __global__ __launch_bounds__(256, 6) void sum_pieces_kernel(GradParams p) {
   }
 }
 
-// Adds the pieces of long runs, in order.
+// Adds the pieces of long runs: a workgroup to a run and 512 columns, the pieces in kJoinWaves equal parts,
+// each part by a wave in order, then the parts in order.
+constexpr int kJoinWaves = 8;
 template <bool kFp32, bool kAdd>
-__global__ __launch_bounds__(64) void join_pieces_kernel(GradParams p) {
-  constexpr int kAhead = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void join_pieces_kernel(GradParams p) {
+  constexpr int kAhead = 8;
+  __shared__ float sums[kJoinWaves][8][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const ListParts parts(p.heads->longs, p.heads->base, kPiece);
   const int total = parts.total();
   for (PairWalk walk(blockIdx.x, gridDim.x, p.hidden); walk.entry < total; walk.go_on()) {
     const LongRun run = p.longs[parts.at(walk.entry)];
-    const int col = walk.block * 512 + 8 * threadIdx.x;
-    if (col >= p.hidden) continue;
+    const int col = walk.block * 512 + 8 * lane;
+    const bool here = col < p.hidden;
+    const int pieces = (run.end - run.begin + kPiece - 1) / kPiece, share = (pieces + kJoinWaves - 1) / kJoinWaves;
+    const int last = min((wave + 1) * share, pieces);
     float s[8] = {};
-    for (int i0 = run.begin; i0 < run.end; i0 += kAhead * kPiece) {
+    for (int k0 = wave * share; k0 < last; k0 += kAhead) {
       float4 q[kAhead][2];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + j * kPiece;
         q[j][0] = q[j][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (i >= run.end) continue;
-        const float4* in = reinterpret_cast<const float4*>(p.parts + part_of(i, i == run.begin) * p.hidden + col);
+        if (k0 + j >= last || !here) continue;
+        const float4* in = reinterpret_cast<const float4*>(p.parts + part_of(run.begin + (k0 + j) * kPiece, k0 + j == 0) * p.hidden + col);
         q[j][0] = in[0];
         q[j][1] = in[1];
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (i0 + j * kPiece >= run.end) break;
+        if (k0 + j >= last) break;
         const float x[8] = {q[j][0].x, q[j][0].y, q[j][0].z, q[j][0].w, q[j][1].x, q[j][1].y, q[j][1].z, q[j][1].w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = s[e] + x[e];
       }
     }
-    write_row<kFp32, kAdd>(p, run.row, col, s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][e][lane] = s[e];
+    __syncthreads();
+    if (wave == 0 && here) {
+      for (int w = 1; w * share < pieces; ++w)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = s[e] + sums[w][e][lane];
+      write_row<kFp32, kAdd>(p, run.row, col, s);
+    }
+    __syncthreads();
   }
 }
 
@@ -618,7 +659,7 @@ struct GradSpace {
     keys = 0;
     order = keys + 2 * round256(4 * tokens);
     hist = order + 2 * round256(4 * tokens);
-    heads = hist + round256(4 * kBins * tiles);
+    heads = hist + round256(4 * kBins * (tiles + 1));
     pieces = heads + round256(sizeof(ListHeads));
     longs = pieces + round256(sizeof(Piece) * tokens);
     parts = longs + round256(sizeof(LongRun) * stretches);
@@ -711,6 +752,10 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
       buffers(pass & 1);
       s.shift = pass * s.bits;
       e = pass == 0 ? launch(sort_count_kernel<true>, s.tiles, kTileThreads, 0) : launch(sort_count_kernel<false>, s.tiles, kTileThreads, 0);
+      if (e == hipSuccess && s.tiles > kManyTiles) {
+        hipLaunchKernelGGL(sum_tiles_kernel, dim3(kBins / 64), dim3(64), 0, stream, s.hist, s.tiles);
+        e = hipGetLastError();
+      }
       if (e == hipSuccess)
         e = pass == 0 ? launch(sort_move_kernel<true>, s.tiles, kTileThreads, 0) : launch(sort_move_kernel<false>, s.tiles, kTileThreads, 0);
     }
@@ -732,12 +777,12 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   p.hidden = a.hidden_dim;
   const int64_t units = static_cast<int64_t>(a.num_tokens) * ((a.hidden_dim + 511) / 512);
   const int64_t sum_grid = (units + 3) / 4 < 32 * cus ? (units + 3) / 4 : 32 * cus;
-  const int64_t join_grid = units / kPiece + 1 < 16 * cus ? units / kPiece + 1 : 16 * cus;
+  const int64_t join_grid = units / kPiece + 1 < 4 * cus ? units / kPiece + 1 : 4 * cus;
   auto sums = [&](auto fp32, auto add) {
     constexpr bool kFp32 = decltype(fp32)::value, kAdd = decltype(add)::value;
     hipLaunchKernelGGL((sum_pieces_kernel<kFp32, kAdd>), dim3(sum_grid), dim3(256), 0, stream, p);
     if (a.num_tokens > kPiece)
-      hipLaunchKernelGGL((join_pieces_kernel<kFp32, kAdd>), dim3(join_grid), dim3(64), 0, stream, p);
+      hipLaunchKernelGGL((join_pieces_kernel<kFp32, kAdd>), dim3(join_grid), dim3(64 * kJoinWaves), 0, stream, p);
   };
   if (a.grad_fp32 && a.accumulate)
     sums(std::true_type{}, std::true_type{});

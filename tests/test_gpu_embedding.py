@@ -95,6 +95,25 @@ def test_gradient_matches_oracle(ua, T, V, H, kind, fp32, accumulate):
     assert np.array_equal(have[untouched], want[untouched])
 
 
+@pytest.mark.parametrize("T,V,H", [(524288, 151936, 8), (524289, 777, 16), (1500000, 300000, 8), (3000000, 3, 8)])
+def test_many_tokens(ua, T, V, H):
+    """The tiles' counts summed by a launch of their own, and runs of a million tokens; fp64 sums on the GPU."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    ids = torch.randint(-1, V + 1, (T,), generator=g, device="cuda", dtype=torch.int32)
+    dout = torch.randn((T, H), generator=g, device="cuda").to(torch.bfloat16)
+    got = ua.embedding_backward(dout, ids, V)
+    ok = (ids >= 0) & (ids < V)
+    at, x = ids[ok].long(), dout[ok].double()
+    want = torch.zeros((V, H), dtype=torch.float64, device="cuda").index_add_(0, at, x)
+    mag = torch.zeros((V, H), dtype=torch.float64, device="cuda").index_add_(0, at, x.abs())
+    count = torch.bincount(at, minlength=V)[:, None]
+    # a piece's 32 tokens, then the pieces one after another, and the scale
+    assert bool(((got.double() - want).abs() <= (34 + count / 32) * U * mag).all())
+    assert torch.equal(got, ua.embedding_backward(dout, ids, V))
+
+
 @pytest.mark.parametrize("T,V,H", [(700, 50, 256), (6000, 200, 64), (30000, 3000, 64)])
 def test_rows_depend_on_their_own_tokens_alone(ua, T, V, H):
     """Other tokens put between, and calls in a row: the same bits for an entry's row."""
@@ -173,6 +192,18 @@ def test_rows_past_2_31_elements(ua):
     ua.embedding_backward(out, ids, V, grad=table)
     assert torch.equal(table[V - 2], last[1]) and torch.equal(table[V - 1], (2 * last[2].float()).to(torch.bfloat16))
     assert not table[:V - 3].any()
+
+
+def test_validation(ua, monkeypatch):
+    import torch
+    monkeypatch.setenv("UATTN_VALIDATE", "1")
+    t = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
+    assert ua.embedding(gu.dev_i32([0, 3, -1]), t).shape == (3, 64)
+    assert ua.embedding_backward(t, gu.dev_i32([0, 3, -1, 2]), 4).shape == (4, 64)
+    with pytest.raises(ua.UattnError):
+        ua.embedding(gu.dev_i32([0, 4]), t)
+    with pytest.raises(ua.UattnError):
+        ua.embedding_backward(t, gu.dev_i32([0, 3, 4, 2]), 4)
 
 
 def test_binding_refuses(ua):

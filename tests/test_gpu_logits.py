@@ -350,6 +350,33 @@ def test_no_rows_and_empty_lists(ua):
     assert torch.equal(same, z)
 
 
+def test_validation(ua, monkeypatch):
+    """UATTN_VALIDATE=1 refuses what is clamped or ignored otherwise."""
+    import torch
+    V = 64
+    z = torch.zeros((2, V), dtype=torch.bfloat16, device="cuda")
+    tok, pen, one = gu.dev_i32([1, 2, 3]), _f32([[1.5, 0, 0]] * 2), _f32([1.0])
+    mask = torch.ones((1, 2), dtype=torch.int32, device="cuda")
+    good = [lambda: ua.logits_process(z, tok, gu.dev_i32([[0, 1, 3], [3, 3, 3]]), pen),
+            lambda: ua.logits_process(z, bias_ids=gu.dev_i32([5]), bias_values=one, bias_rows=gu.dev_i32([[0, 1], [0, 0]])),
+            lambda: ua.logits_process(z, mask=mask, mask_rows=gu.dev_i32([0, -1])),
+            lambda: ua.logprob_backward(z, gu.dev_i32([0, V - 1]), _f32([1, 1]))]
+    bad = [lambda: ua.logits_process(z, tok, gu.dev_i32([[0, 1, 4], [0, 0, 0]]), pen),
+           lambda: ua.logits_process(z, tok, gu.dev_i32([[0, 2, 1], [0, 0, 0]]), pen),
+           lambda: ua.logits_process_backward(z, z, tok, gu.dev_i32([[-1, 0, 1], [0, 0, 0]]), pen),
+           lambda: ua.logits_process(z, bias_ids=gu.dev_i32([5]), bias_values=one, bias_rows=gu.dev_i32([[0, 2], [0, 0]])),
+           lambda: ua.logits_process(z, mask=mask, mask_rows=gu.dev_i32([0, 1])),
+           lambda: ua.logprob_backward(z, gu.dev_i32([0, V]), _f32([1, 1]))]
+    for f in good + bad:
+        f()
+    monkeypatch.setenv("UATTN_VALIDATE", "1")
+    for f in good:
+        f()
+    for f in bad:
+        with pytest.raises(ua.UattnError):
+            f()
+
+
 def test_binding_refuses(ua):
     import torch
     V = 64
