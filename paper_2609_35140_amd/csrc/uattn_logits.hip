@@ -7,13 +7,14 @@
 //   x = x + bias (the last entry of the row's list that names v);  masked: x = -inf
 // in fp32 (the division as a product with 1 / repetition), rounded to bf16 once.
 //
-// A workgroup takes one stretch of kStretch entries of up to kMaxRows consecutive
-// rows.  It counts the history's tokens that fall into the stretch in LDS (whole
-// numbers, so the order of the atomics does not show) and streams the stretch.  Rows
-// of an update are successive prefixes of a sequence: where a row's history is the
-// one before it and some more, only the new tokens are counted, and most of them fall
-// into other stretches.  Counts do not depend on how they came about, so a decode
-// step's row and the update's row of the same prefix get the same bits.
+// A workgroup takes one stretch of up to 8192 entries (the vocabulary in equal parts,
+// sixteen entries to a thread) of up to kMaxRows consecutive rows.  It counts the
+// history's tokens that fall into the stretch in LDS (whole numbers, so the order of
+// the atomics does not show) and streams the stretch.  Rows of an update are
+// successive prefixes of a sequence: where a row's history is the one before it and
+// some more, only the new tokens are counted, and most of them fall into other
+// stretches.  Counts do not depend on how they came about, so a decode step's row and
+// the update's row of the same prefix get the same bits.
 #include <type_traits>
 
 #include "uattn_internal.h"
@@ -22,9 +23,10 @@
 namespace uattn {
 namespace {
 
-constexpr int kLogitsThreads = 512;
+constexpr int kLogitsThreads = 512;  // at most
 constexpr int kLogitsVecs = 2;
-constexpr int kStretch = kLogitsThreads * kLogitsVecs * 8;
+constexpr int kThreadEntries = 8 * kLogitsVecs;
+constexpr int kMostEntries = kLogitsThreads * kThreadEntries;  // of a stretch
 constexpr int kMaxRows = 16;
 constexpr uint32_t kPrompt = 0x80000000u;  // of a count: the entry occurs in the prompt
 constexpr int32_t kNoBias = INT32_MIN;     // of the bias table: as a float, -0, which changes no sum
@@ -55,14 +57,14 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
 }
 
 template <bool kGrad, bool kBias>
-__global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) {
+__global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(LogitsParams p) {
   // counts, and behind them the biases (in their place where the counts serve one row alone)
   extern __shared__ __align__(16) uint32_t table[];
-  int32_t* bias_table = reinterpret_cast<int32_t*>(table) + (p.rows > 1 ? kStretch : 0);
-  const int tid = threadIdx.x, lane = tid & 63;
+  int32_t* bias_table = reinterpret_cast<int32_t*>(table) + (p.rows > 1 ? blockDim.x * kThreadEntries : 0);
+  const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x, stretch = threads * kThreadEntries;
   const int64_t unit = p.first + static_cast<int64_t>(blockIdx.x);
   const int64_t row0 = unit / p.stretches * p.rows;
-  const int v0 = static_cast<int>(unit % p.stretches) * kStretch, n = min(kStretch, p.vocab - v0);
+  const int v0 = static_cast<int>(unit % p.stretches) * stretch, n = min(stretch, p.vocab - v0);
   const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows), p.num_rows - row0));
 
   // Lane r of every wave keeps row r's arguments; the loops below read them from there.
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
     const uint8_t* mask = reinterpret_cast<const uint8_t*>(p.mask + m * p.mask_stride) + v0 / 8;
 #pragma unroll
     for (int i = 0; i < kLogitsVecs; ++i) {
-      const int piece = tid + i * kLogitsThreads, e0 = 8 * piece;
+      const int piece = tid + i * threads, e0 = 8 * piece;
       w[i] = u32x4{0, 0, 0, 0};
       keep[i] = 0xFF;
       if (e0 + 8 <= n)
@@ -120,15 +122,15 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
   };
   auto count = [&](int lo, int hi, int response) {
     constexpr int kAhead = 4;
-    for (int i0 = lo + tid; i0 < hi; i0 += kAhead * kLogitsThreads) {
+    for (int i0 = lo + tid; i0 < hi; i0 += kAhead * threads) {
       int token[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) token[u] = i0 + u * kLogitsThreads < hi ? p.tokens[i0 + u * kLogitsThreads] : -1;
+      for (int u = 0; u < kAhead; ++u) token[u] = i0 + u * threads < hi ? p.tokens[i0 + u * threads] : -1;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const uint32_t v = static_cast<uint32_t>(token[u]) - v0;
         if (v >= static_cast<uint32_t>(n)) continue;
-        if (i0 + u * kLogitsThreads < response)
+        if (i0 + u * threads < response)
           atomicOr(&table[v], kPrompt);
         else
           atomicAdd(&table[v], 1);
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
   u32x4 next_z[kLogitsVecs];
   bool have_z[kLogitsVecs] = {};
   auto load_z = [&](int r, int i) {
-    const int piece = tid + i * kLogitsThreads;
+    const int piece = tid + i * threads;
     const uint16_t* z = p.logits + (row0 + r) * p.logits_stride + v0;
     u32x4 q = {0, 0, 0, 0};
     if (8 * piece + 8 <= n)
@@ -174,8 +176,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
       if (at < 0) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kStretch / 4; e += kLogitsThreads)
-          reinterpret_cast<u32x4*>(table)[e + tid] = u32x4{0, 0, 0, 0};
+        for (int e = 0; e < kThreadEntries / 4; ++e) reinterpret_cast<u32x4*>(table)[e * threads + tid] = u32x4{0, 0, 0, 0};
         __syncthreads();
         count(lo, hi, response);
         __syncthreads();
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
     if (actives >> r & 1) {
       const float mul = lane_float(rep, r), inv = 1.f / mul, f = lane_float(freq, r), q = lane_float(pres, r);
       auto counts = [&](int i, uint32_t (&seen)[8]) {
-        const u32x4* t = reinterpret_cast<const u32x4*>(table) + 2 * (tid + i * kLogitsThreads);
+        const u32x4* t = reinterpret_cast<const u32x4*>(table) + 2 * (tid + i * threads);
         const u32x4 a = t[0], b = t[1];
         uint32_t any = 0;
 #pragma unroll
@@ -244,25 +245,34 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
       const int lo = lane_int(bias_begin, r), hi = lane_int(bias_end, r);
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < kStretch / 4; e += kLogitsThreads)
-        reinterpret_cast<u32x4*>(bias_table)[e + tid] = u32x4{kPrompt, kPrompt, kPrompt, kPrompt};
+      for (int e = 0; e < kThreadEntries / 4; ++e)
+        reinterpret_cast<u32x4*>(bias_table)[e * threads + tid] = u32x4{kPrompt, kPrompt, kPrompt, kPrompt};
       __syncthreads();
-      // the last entry that names v wins its place; then each place takes its winner's value
-      for (int i = lo + tid; i < hi; i += kLogitsThreads) {
+      // the last entry that names v wins its place
+      for (int i = lo + tid; i < hi; i += threads) {
         const uint32_t v = static_cast<uint32_t>(i == lo + tid ? first_id : p.bias_ids[i]) - v0;
         if (v < static_cast<uint32_t>(n)) atomicMax(&bias_table[v], i);
       }
       __syncthreads();
-      for (int e = tid; e < kStretch; e += kLogitsThreads) {
-        const int32_t i = bias_table[e];
-        if (i != kNoBias) bias_table[e] = __float_as_int(p.bias_values[i]);
+      if (hi - lo <= threads) {
+        // an entry to a thread: the winners put their values there, once all have looked
+        const uint32_t v = static_cast<uint32_t>(first_id) - v0;
+        const bool wins = v < static_cast<uint32_t>(n) && bias_table[v] == lo + tid;
+        __syncthreads();
+        if (wins) bias_table[v] = __float_as_int(p.bias_values[lo + tid]);
+      } else {
+        // longer lists: each place takes its winner's value (a value's bits could be another entry's number)
+        for (int e = tid; e < stretch; e += threads) {
+          const int32_t i = bias_table[e];
+          if (i != kNoBias) bias_table[e] = __float_as_int(p.bias_values[i]);
+        }
       }
       __syncthreads();
     }
     if (kBias && lane_int(bias_begin, r) < lane_int(bias_end, r)) {
 #pragma unroll
       for (int i = 0; i < kLogitsVecs; ++i) {
-        const float4* t = reinterpret_cast<const float4*>(bias_table) + 2 * (tid + i * kLogitsThreads);
+        const float4* t = reinterpret_cast<const float4*>(bias_table) + 2 * (tid + i * threads);
         const float4 a = t[0], b = t[1];
         const float add[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -273,7 +283,7 @@ __global__ __launch_bounds__(kLogitsThreads) void logits_kernel(LogitsParams p) 
     const bool masked = lane_int(mask_row, r) >= 0;
 #pragma unroll
     for (int i = 0; i < kLogitsVecs; ++i) {
-      const int piece = tid + i * kLogitsThreads, e0 = 8 * piece;
+      const int piece = tid + i * threads, e0 = 8 * piece;
       if (e0 >= n) break;
       if (masked) {
 #pragma unroll
@@ -310,21 +320,22 @@ hipError_t launch_logits(const LogitsLaunch& a, bool grad, hipStream_t stream) {
   p.num_tokens = a.num_tokens;
   p.num_bias = a.num_bias;
   p.num_masks = a.num_masks;
-  p.stretches = (a.vocab - 1) / kStretch + 1;
+  p.stretches = (a.vocab - 1) / kMostEntries + 1;
+  const int threads = ((a.vocab - 1) / p.stretches / kThreadEntries / 64 + 1) * 64;  // equal parts, whole waves
   p.stream = streams(a.num_rows, a.vocab);
   // few rows are spread over all CUs, many share their counts
   const int64_t share = static_cast<int64_t>(a.num_rows) * p.stretches / (16 * device_cus());
   p.rows = static_cast<int>(share < 1 ? 1 : share > kMaxRows ? kMaxRows : share);
   const int64_t groups = (static_cast<int64_t>(a.num_rows) + p.rows - 1) / p.rows;
-  const size_t lds = sizeof(uint32_t) * kStretch * (a.bias_rows != nullptr && p.rows > 1 ? 2 : 1);
-  return launch_parts(groups * p.stretches, kLogitsThreads, [&](int first, unsigned n) {
+  const size_t lds = sizeof(uint32_t) * threads * kThreadEntries * (a.bias_rows != nullptr && p.rows > 1 ? 2 : 1);
+  return launch_parts(groups * p.stretches, threads, [&](int first, unsigned n) {
     p.first = first;
     if (grad)
-      hipLaunchKernelGGL((logits_kernel<true, false>), dim3(n), dim3(kLogitsThreads), lds, stream, p);
+      hipLaunchKernelGGL((logits_kernel<true, false>), dim3(n), dim3(threads), lds, stream, p);
     else if (a.bias_rows != nullptr)
-      hipLaunchKernelGGL((logits_kernel<false, true>), dim3(n), dim3(kLogitsThreads), lds, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, true>), dim3(n), dim3(threads), lds, stream, p);
     else
-      hipLaunchKernelGGL((logits_kernel<false, false>), dim3(n), dim3(kLogitsThreads), lds, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, false>), dim3(n), dim3(threads), lds, stream, p);
   });
 }
 

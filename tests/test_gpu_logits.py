@@ -148,6 +148,20 @@ def test_earlier_entry_does_not_win_over_a_value_like_its_place(ua):
     assert got[0, 5] == 1 and got[0, 6] == 1 and got[1, 5] == 1 and got[1, 6] == 10
 
 
+@pytest.mark.parametrize("T,V,M", [(3, 100, 64), (3, 100, 65), (2, 9000, 320), (2, 9000, 321), (40, 9000, 1500), (1, 200, 5000)])
+def test_bias_lists_around_the_threads(ua, T, V, M):
+    """Lists of as many entries as a workgroup has threads, and more; the same id many times."""
+    g = inputs.rng(346, T, V, M)
+    z = inputs.normal_bf16((T, V), 1.0, 347, T, V)
+    ids, vals = g.integers(-2, V + 2, M).astype(np.int32), g.integers(-3, 4, M).astype(np.float32)
+    rows = np.tile(np.array([[0, M]], dtype=np.int32), (T, 1))
+    rows[T // 2] = (M // 3, M)
+    kw = dict(bias_ids=ids, bias_values=vals, bias_rows=rows)
+    want, mag = oracle.logits_process_fp64(oracle.bf16_to_f64(z), **kw)
+    got = gu.host_f64(ua.logits_process(_rows(z)[:, :V], **_device(kw, BIAS)))
+    assert np.all(np.abs(got - want) <= (HALF + U) * np.abs(want) + 8 * U * mag)
+
+
 @pytest.mark.parametrize("T,V", [(700, 20011), (90, 151936)])
 def test_histories_that_go_on_from_row_to_row(ua, T, V):
     """Many rows whose histories grow by none, one or several tokens, change their sequence, or shrink: what a row alone gets."""
