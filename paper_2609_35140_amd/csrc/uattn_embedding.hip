@@ -73,9 +73,9 @@ __global__ __launch_bounds__(kEmbedWaves * 64) void embedding_kernel(EmbeddingPa
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;  // of a pass of a radix sort, at most
 constexpr int kPiece = 32;                 // tokens a wave sums
 // Up to kSmall tokens are sorted in one launch, by kBuckets workgroups in LDS: the b-th takes the ids
-// v with v % kBuckets = b, so that frequent neighbours are spread.  (One workgroup for all: 16,000
-// tokens 62 us.  The launches for more tokens take about 40, whatever their number up to 65,536.)
-constexpr int kSmall = 16384, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kBuckets = 32;
+// v with v % kBuckets = b, so that frequent neighbours are spread.  (16,000 tokens: 62 us by one workgroup,
+// 18 by 64; the launches for more tokens take about 35, whatever their number up to 65,536.)
+constexpr int kSmall = 16384, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64, kBuckets = 64;
 constexpr int kSmallRounds = kSmall / kSmallThreads;
 constexpr int kTileThreads = 512, kTileWaves = kTileThreads / 64;
 constexpr int kTile = 2048, kTileRounds = kTile / kTileThreads;
@@ -215,8 +215,9 @@ struct ListParts {
   int32_t until, count, base;
   __device__ __forceinline__ ListParts(const int32_t* counts, const int32_t* bases, int divide) {
     const int lane = threadIdx.x & 63;
-    count = lane < kBuckets ? counts[lane] : 0;
-    base = lane < kBuckets ? bases[lane] / divide : 0;
+    static_assert(kBuckets == 64, "a lane to a part");
+    count = counts[lane];
+    base = bases[lane] / divide;
     until = count;
 #pragma unroll
     for (int d = 1; d < kBuckets; d *= 2) {
@@ -227,7 +228,7 @@ struct ListParts {
   __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(until, kBuckets - 1); }
   // where the k-th entry of all stands
   __device__ __forceinline__ int at(int k) const {
-    const int b = __popcll(__ballot((threadIdx.x & 63) < kBuckets && until <= k));
+    const int b = __popcll(__ballot(until <= k));
     return k - __builtin_amdgcn_readlane(until, b) + __builtin_amdgcn_readlane(count, b) + __builtin_amdgcn_readlane(base, b);
   }
 };
@@ -690,10 +691,11 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   z.grad = a.grad;
   z.row_pieces = a.grad_stride * size / 16;
   z.pieces = a.hidden_dim * size / 16;
-  // workgroups that write zeros beside `sorters` that sort, `threads` each: all CUs' threads
+  // workgroups of `threads` that write zeros: a row to a wave, in the order they start, so that neighbours are
+  // written together (151,936 x 4096 fp32: 482 us a call so, 514 with two to a CU that walk the table)
   auto zeroers = [&](int threads) {
     const int64_t waves = threads / 64, blocks = (z.end - z.begin + waves - 1) / waves;
-    const int64_t most = static_cast<int64_t>(cus) * 2048 / threads;
+    const int64_t most = static_cast<int64_t>(cus) * 131072 / threads;
     return static_cast<unsigned>(blocks < most ? blocks : most);
   };
   if (a.num_tokens == 0) {
