@@ -281,7 +281,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p)
   }
   uint16_t* order = reinterpret_cast<uint16_t*>(keys + p.num_tokens);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint64_t below = (uint64_t{1} << lane) - 1;
+  const uint64_t below = (uint64_t{1} << lane) - 1;  // the lanes before this one
   int rounds = (p.num_tokens + kSmallThreads - 1) / kSmallThreads, begin = wave * rounds * 64 + lane;
   uint32_t key[kSmallRounds];
   int32_t from[kSmallRounds], at[kSmallRounds];
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(SortParams p)
     for (int i = tid; i < kSmallWaves * kBins; i += kSmallThreads) seen[0][i] = 0;
     __syncthreads();
     for (int r = 0; r < rounds; ++r) {
-        const int i = begin + r * 64;
+      const int i = begin + r * 64;
       key[r] = i < n ? keys[i] : 0;
       from[r] = i < n ? order[i] : 0;
       at[r] = rank_in_wave(seen[wave], key[r] >> shift & low, i < n, p.bits, lane);
@@ -690,7 +690,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   ZeroParams z{};
   z.grad = a.grad;
   z.row_pieces = a.grad_stride * size / 16;
-  z.pieces = a.hidden_dim * size / 16;
+  z.pieces = static_cast<int32_t>(static_cast<int64_t>(a.hidden_dim) * size / 16);
   // workgroups of `threads` that write zeros: a row to a wave, in the order they start, so that neighbours are
   // written together (151,936 x 4096 fp32: 482 us a call so, 514 with two to a CU that walk the table)
   auto zeroers = [&](int threads) {
