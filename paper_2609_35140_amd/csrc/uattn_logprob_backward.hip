@@ -3,12 +3,12 @@
 //   dlogits[v] = dlogp * inv_temperature * (1[v = target] - p_v),  p = softmax(logits * inv_temperature)
 //
 // One workgroup per row.  With k = inv_temperature * log2(e) every thread keeps a
-// running reference R = max x * k and the sum of exp2(fma(x, k, -R)); R's rounding
-// is common to all terms and leaves with the division.  The target's own
-// exponential is left out of the sum and added last, so that 1 - p of the target is
-// the others' sum over the whole one: their difference from 1 would leave no digits
-// where the target is nearly certain.  The order of the sum depends on the
-// vocabulary alone.
+// running maximum m and the sum of exp2((x - m) k); the difference comes first, so
+// that logits near the end of bf16's range (a row masked by its lowest value) do not
+// overflow.  The target's own exponential is left out of the sum and added last, so
+// that 1 - p of the target is the others' sum over the whole one: their difference
+// from 1 would leave no digits where the target is nearly certain.  The order of the
+// sum depends on the vocabulary alone.
 #include <type_traits>
 
 #include "uattn_internal.h"
@@ -32,19 +32,18 @@ struct LogprobGradParams {
 __device__ __forceinline__ float neg_infinity() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A sum of exponentials relative to 2^ref.
-struct RefSum {
-  float ref, sum;
+// A maximum and the sum of exponentials relative to it.
+struct MaxSum {
+  float m, sum;
 };
-__device__ __forceinline__ float rebase(float from, float to) {
-  return from == neg_infinity() ? 0.f : exp2_of(from - to);
+// What is subtracted from the logits: a maximum of -inf (nothing but masked entries) subtracts nothing.
+__device__ __forceinline__ float shift_of(float m) { return m == neg_infinity() ? 0.f : m; }
+// A sum relative to `from`, relative to `to` (to >= from).
+__device__ __forceinline__ float rebase(float from, float to, float k) { return exp2_of((from - shift_of(to)) * k); }
+__device__ __forceinline__ MaxSum combine(MaxSum a, MaxSum b, float k) {
+  const float m = fmaxf(a.m, b.m);
+  return MaxSum{m, a.sum * rebase(a.m, m, k) + b.sum * rebase(b.m, m, k)};
 }
-__device__ __forceinline__ RefSum combine(RefSum a, RefSum b) {
-  const float r = fmaxf(a.ref, b.ref);
-  return RefSum{r, a.sum * rebase(a.ref, r) + b.sum * rebase(b.ref, r)};
-}
-// What is subtracted from the exponents: a reference of -inf (nothing but masked entries) subtracts nothing.
-__device__ __forceinline__ float shift_of(float ref) { return ref == neg_infinity() ? 0.f : ref; }
 
 // Bound by memory.  The row stays in registers between its sum and its gradient (kVecs 16-byte pieces to
 // a thread, all requested at once): it is read once and written once (4100 rows of 151,936: 481 us, 5.2 TB/s;
@@ -53,7 +52,7 @@ template <int kThreads, int kVecs>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParams p) {
   constexpr int kWaves = kThreads / 64;
   constexpr u32x4 kNegInf = {0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};
-  __shared__ RefSum parts[kWaves];
+  __shared__ MaxSum parts[kWaves];
   const int64_t row = p.first + static_cast<int64_t>(blockIdx.x);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint16_t* x = p.logits + row * p.stride;
@@ -75,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
     w[i] = kNegInf;
     if (v0 < pieces && v0 + lane < pieces) w[i] = load16(x, 0, v0 + lane);
   }
-  RefSum acc{neg_infinity(), 0.f};
+  MaxSum acc{neg_infinity(), 0.f};
   // adds kN pieces, which begin at v0 + j * kThreads
   auto add = [&](auto n_const, const u32x4* q, int v0) {
     constexpr int kN = decltype(n_const)::value;
@@ -84,14 +83,15 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
     for (int j = 0; j < kN; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(bf16_lo(q[j][e]), bf16_hi(q[j][e])));
-    const float ref = fmaxf(acc.ref, m * p.k), shift = shift_of(ref);
+    m = fmaxf(acc.m, m);
+    const float shift = shift_of(m);
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
       float t[8];
       unpack8(q[j], t);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = exp2_of(__builtin_fmaf(t[e], p.k, -shift));
+      for (int e = 0; e < 8; ++e) t[e] = exp2_of((t[e] - shift) * p.k);
       const int at = y_piece - (v0 + j * kThreads);
       if (at >= 0 && at < 64) {
 #pragma unroll
@@ -99,8 +99,8 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
       }
       sum = sum + (((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
     }
-    acc.sum = acc.sum * rebase(acc.ref, ref) + sum;
-    acc.ref = ref;
+    acc.sum = acc.sum * rebase(acc.m, m, p.k) + sum;
+    acc.m = m;
   };
   constexpr int kStep = 4;
 #pragma unroll
@@ -122,29 +122,29 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
     add(std::integral_constant<int, 1>{}, &q, v0);
   }
   if (tail < p.vocab) {
-    const float t = bf16_lo(x[tail]), ref = fmaxf(acc.ref, t * p.k);
-    acc.sum = acc.sum * rebase(acc.ref, ref) + (tail == y ? 0.f : exp2_of(__builtin_fmaf(t, p.k, -shift_of(ref))));
-    acc.ref = ref;
+    const float t = bf16_lo(x[tail]), m = fmaxf(acc.m, t);
+    acc.sum = acc.sum * rebase(acc.m, m, p.k) + (tail == y ? 0.f : exp2_of((t - shift_of(m)) * p.k));
+    acc.m = m;
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1)
-    acc = combine(acc, RefSum{__shfl_xor(acc.ref, off, 64), __shfl_xor(acc.sum, off, 64)});
+    acc = combine(acc, MaxSum{__shfl_xor(acc.m, off, 64), __shfl_xor(acc.sum, off, 64)}, p.k);
   if constexpr (kWaves > 1) {
     if (lane == 0) parts[wave] = acc;
     __syncthreads();
     acc = parts[0];
 #pragma unroll
-    for (int u = 1; u < kWaves; ++u) acc = combine(acc, parts[u]);
+    for (int u = 1; u < kWaves; ++u) acc = combine(acc, parts[u], p.k);
   }
-  const float shift = shift_of(acc.ref), g = dlogp * p.it;
-  const float of_target = known ? exp2_of(__builtin_fmaf(bf16_lo(x[y]), p.k, -shift)) : 0.f;
+  const float shift = shift_of(acc.m), g = dlogp * p.it;
+  const float of_target = known ? exp2_of((bf16_lo(x[y]) - shift) * p.k) : 0.f;
   const float inv = known ? 1.f / (acc.sum + of_target) : __builtin_nanf("");
   const float scale = -g * inv, at_target = g * (acc.sum * inv);
   auto put = [&](const u32x4& q, int v0) {
     float t[8];
     unpack8(q, t);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = scale * exp2_of(__builtin_fmaf(t[e], p.k, -shift));
+    for (int e = 0; e < 8; ++e) t[e] = scale * exp2_of((t[e] - shift) * p.k);
     const int at = y_piece - v0;
     if (at >= 0 && at < 64) {
 #pragma unroll
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
     put(q, v0);
   }
   if (tail < p.vocab) {
-    const float d = tail == y ? at_target : scale * exp2_of(__builtin_fmaf(bf16_lo(x[tail]), p.k, -shift));
+    const float d = tail == y ? at_target : scale * exp2_of((bf16_lo(x[tail]) - shift) * p.k);
     out[tail] = static_cast<uint16_t>(bf16_pair(d, d));
   }
 }

@@ -288,6 +288,39 @@ def test_logprob_gradient_of_special_rows(ua):
     assert got[0].tolist() == [-1.0, -1.0, 3.0, -1.0]
 
 
+@pytest.mark.parametrize("V", [16, 1003, 70000])
+@pytest.mark.parametrize("it", [0.5, 1.0, 3.0])
+def test_logprob_gradient_at_the_ends_of_bf16(ua, V, it):
+    """Entries masked by bf16's lowest value, a row of nothing else (uniform), and one whose maximum is its largest."""
+    z = inputs.normal_bf16((4, V), 2.0, 348, V)
+    z[0, ::2] = 0xFF7F
+    z[1] = 0xFF7F
+    z[2, 3] = 0x7F7F
+    z[3, 1:] = 0xFF80
+    tg, dl = np.array([1, 2, 3, 0]), np.array([1.0, -2.0, 0.5, 1.0], dtype=np.float32)
+    got = gu.host_f64(ua.logprob_backward(_rows(z)[:, :V], gu.dev_i32(tg), _f32(dl), it))
+    want, err = oracle.logprob_backward_fp64(oracle.bf16_to_f64(z), tg, dl, it)
+    # the exponents of such differences round by more than the exponential's range: those entries are 0 on both sides
+    far = np.where(np.abs(want) < 1e-30, 1e-30, 0.0)
+    assert np.all(np.abs(got - want) <= (HALF + U) * np.abs(want) + np.where(np.isfinite(err), np.minimum(err, 1.0), 0) * (far == 0) + far)
+    assert not got[0, ::2].any() and abs(got[1, 0] + dl[1] * it / V) <= HALF * abs(dl[1]) * it / V * 1.01
+
+
+@pytest.mark.parametrize("T,V", [(1, 33), (5, 1000), (20, 9000)])
+def test_a_mask_to_every_row(ua, T, V):
+    """mask_rows left out: row t has mask t; the masks' rows stand further apart than they are long."""
+    import torch
+    z = inputs.normal_bf16((T, V), 2.0, 349, T, V)
+    words = (V + 31) // 32
+    wide = torch.from_numpy(inputs.rng(355, T, V).integers(-2 ** 31, 2 ** 31, (T + 2, words + 5)).astype(np.int32)).cuda()
+    mask = wide[:, :words]
+    want, _ = oracle.logits_process_fp64(oracle.bf16_to_f64(z), mask=mask.cpu().numpy())
+    got = gu.host_f64(ua.logits_process(_rows(z)[:, :V], mask=mask))
+    assert np.array_equal(got, want)
+    d = oracle.logits_process_backward_fp64(oracle.bf16_to_f64(z), oracle.bf16_to_f64(z), mask=mask.cpu().numpy())
+    assert np.array_equal(gu.host_f64(ua.logits_process_backward(_rows(z)[:, :V], _rows(z)[:, :V], mask=mask)), d)
+
+
 def test_rows_do_not_depend_on_the_batch(ua):
     import torch
     T, V = 37, 50257
