@@ -57,11 +57,13 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint16_t* x = p.logits + row * p.stride;
   uint16_t* out = p.out + row * p.out_stride;
-  const int y = p.targets[row], pieces = p.vocab / 8, tail = 8 * pieces + tid;
+  const int y = p.targets[row], pieces = p.vocab / 8;
+  const bool has_tail = tid < p.vocab % 8;  // an entry behind the pieces: the place `tail`
+  const int tail = 8 * pieces + (tid & 7);
   const float dlogp = p.dlogp[row];
   if (dlogp == 0.f) {
     for (int v = tid; v < pieces; v += kThreads) store16(out, v, u32x4{0, 0, 0, 0});
-    if (tail < p.vocab) out[tail] = 0;
+    if (has_tail) out[tail] = 0;
     return;
   }
   const bool known = y >= 0 && y < p.vocab;
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
     if (v0 + lane < pieces) q = load16(x, 0, v0 + lane);
     add(std::integral_constant<int, 1>{}, &q, v0);
   }
-  if (tail < p.vocab) {
+  if (has_tail) {
     const float t = bf16_lo(x[tail]), m = fmaxf(acc.m, t);
     acc.sum = acc.sum * rebase(acc.m, m, p.k) + (tail == y ? 0.f : exp2_of((t - shift_of(m)) * p.k));
     acc.m = m;
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParam
     if (v0 + lane < pieces) q = load16(x, 0, v0 + lane);
     put(q, v0);
   }
-  if (tail < p.vocab) {
+  if (has_tail) {
     const float d = tail == y ? at_target : scale * exp2_of((bf16_lo(x[tail]) - shift) * p.k);
     out[tail] = static_cast<uint16_t>(bf16_pair(d, d));
   }

@@ -343,6 +343,24 @@ def test_rows_do_not_depend_on_the_batch(ua):
         assert torch.equal(bs.view(torch.int16), back[at].view(torch.int16))
 
 
+def test_widest_vocabulary(ua):
+    """A vocabulary just below 2^31, odd: one row is 4 GB, and places behind its last entry have no 32-bit number.
+
+    Equal logits: the fp32 sum of the V - 1 others is within a few 2^-24 of 2^31, so every gradient but the target's
+    rounds to -2^-31 and the target's to 1.
+    """
+    import torch
+    V = 2 ** 31 - 9
+    z = torch.zeros((1, V + 1), dtype=torch.bfloat16, device="cuda")[:, :V]
+    got = ua.logprob_backward(z, gu.dev_i32([V - 1]), _f32([1.0]))
+    assert got[0, V - 1].item() == 1.0 and not (got[0, :V - 1] != -2.0 ** -31).any()
+    del got
+    got = ua.logits_process(z, bias_ids=gu.dev_i32([V - 1, 8192]), bias_values=_f32([2.0, 3.0]), bias_rows=gu.dev_i32([[0, 2]]))
+    assert got[0, V - 1].item() == 2.0 and got[0, 8192].item() == 3.0 and int((got != 0).sum()) == 2
+    del got, z
+    torch.cuda.empty_cache()
+
+
 def test_captured_and_replayed(ua):
     import torch
     T, V = 6, 9001
