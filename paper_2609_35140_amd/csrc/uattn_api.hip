@@ -714,9 +714,10 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
   if (!logits || !targets || !dlogp || !dlogits || !aligned16(logits) || !aligned16(dlogits)) return UATTN_EINVAL;
   if (validate_env()) {
     Copied<int32_t> tg(targets, num_rows);
-    if (tg.host == nullptr) return UATTN_EINVAL;
+    Copied<float> dl(dlogp, num_rows);
+    if (tg.host == nullptr || dl.host == nullptr) return UATTN_EINVAL;
     for (int32_t t = 0; t < num_rows; ++t)
-      if (tg.host[t] < 0 || tg.host[t] >= vocab) return UATTN_EINVAL;
+      if (dl.host[t] != 0.f && (tg.host[t] < 0 || tg.host[t] >= vocab)) return UATTN_EINVAL;
   }
   uattn::LogprobBackwardLaunch a;
   a.logits = logits;

@@ -425,7 +425,8 @@ def test_validation(ua, monkeypatch):
     good = [lambda: ua.logits_process(z, tok, gu.dev_i32([[0, 1, 3], [3, 3, 3]]), pen),
             lambda: ua.logits_process(z, bias_ids=gu.dev_i32([5]), bias_values=one, bias_rows=gu.dev_i32([[0, 1], [0, 0]])),
             lambda: ua.logits_process(z, mask=mask, mask_rows=gu.dev_i32([0, -1])),
-            lambda: ua.logprob_backward(z, gu.dev_i32([0, V - 1]), _f32([1, 1]))]
+            lambda: ua.logprob_backward(z, gu.dev_i32([0, V - 1]), _f32([1, 1])),
+            lambda: ua.logprob_backward(z, gu.dev_i32([-1, V]), _f32([0, 0]))]  # padded rows: their targets are not used
     bad = [lambda: ua.logits_process(z, tok, gu.dev_i32([[0, 1, 4], [0, 0, 0]]), pen),
            lambda: ua.logits_process(z, tok, gu.dev_i32([[0, 2, 1], [0, 0, 0]]), pen),
            lambda: ua.logits_process_backward(z, z, tok, gu.dev_i32([[-1, 0, 1], [0, 0, 0]]), pen),
