@@ -458,8 +458,8 @@ uattn_status uattn_residual_norm_backward(const void* dy, const void* dresidual_
  *   table   [vocab, table_stride] bf16, first hidden_dim used
  *   scale   finite
  *   out     [num_tokens, out_stride] bf16, first hidden_dim written
- *   hidden_dim a multiple of 8; strides >= hidden_dim and multiples of 8
- *   elements; pointers 16-byte aligned.
+ *   hidden_dim a multiple of 8, at most 2^20 (UATTN_EUNSUPPORTED above);
+ *   strides >= hidden_dim and multiples of 8 elements; pointers 16-byte aligned.
  */
 uattn_status uattn_embedding(const int32_t* ids, const void* table, int64_t table_stride, float scale,
                              int32_t num_tokens, int32_t vocab, int32_t hidden_dim, void* out, int64_t out_stride,
@@ -478,15 +478,17 @@ size_t uattn_embedding_backward_workspace_bytes(int32_t num_tokens, int32_t hidd
  *   grad[v] = scale * sum over t with ids[t] = v of dout[t]   (+ grad[v] with accumulate)
  *
  *   dout        [num_tokens, dout_stride] bf16, first hidden_dim used
- *   ids         [num_tokens] int32; ids outside [0, vocab) add nothing
+ *   ids         [num_tokens] int32; ids outside [0, vocab) add nothing (those of
+ *               vocab or more are refused under UATTN_VALIDATE)
  *   grad        [vocab, grad_stride] bf16 (grad_fp32 0) or fp32 (grad_fp32 1),
  *               first hidden_dim of every row written.  accumulate 0: rows no id
  *               names become zeros; accumulate 1: they are left as they were
  *   workspace   at least uattn_embedding_backward_workspace_bytes bytes, 16-byte
  *               aligned, no initial contents needed; calls sharing a workspace must
  *               be ordered on one stream
- *   num_tokens at most 2^30 (UATTN_EUNSUPPORTED above); hidden_dim a multiple of
- *   8; dout_stride a multiple of 8, grad_stride of 16 bytes; pointers 16-byte aligned.
+ *   num_tokens at most 2^30, hidden_dim 2^20 (UATTN_EUNSUPPORTED above);
+ *   hidden_dim and dout_stride multiples of 8, grad_stride of 16 bytes; pointers
+ *   16-byte aligned.
  *
  * The tokens are sorted by id; an entry's rows are added in ascending order of t
  * in fp32, 32 at a time, then these sums (in eight equal parts, each in order),
@@ -530,6 +532,9 @@ uattn_status uattn_embedding_backward(const void* dout, int64_t dout_stride, con
  *                itself, with the same stride)
  *   strides      >= vocab and multiples of 8 (mask_stride >= ceil(vocab / 32) words);
  *                logits and out 16-byte aligned
+ *   num_tokens, num_bias   at most 2^30 (UATTN_EUNSUPPORTED above)
+ *
+ * Ranges that need clamping and masks of num_masks or more are refused under UATTN_VALIDATE.
  *
  * A row whose mask allows nothing is -inf everywhere (uattn_logprob gives NaN for it).
  */

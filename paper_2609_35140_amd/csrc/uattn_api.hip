@@ -64,6 +64,9 @@ bool all_below(const int32_t* dev, int32_t n, int32_t limit) {
 bool norm_width_ok(int32_t hidden_dim) { return hidden_dim % 8 == 0 && hidden_dim <= 16384; }
 
 constexpr int32_t kMaxSortedTokens = 1 << 30;
+// Past these the kernels' 32-bit columns of a row, and places in the lists of tokens and biases, could overflow.
+constexpr int32_t kMaxEmbeddingWidth = 1 << 20;
+constexpr int32_t kMaxListed = 1 << 30;
 
 // Ranges [begin, end) of `width` columns: column 0 to the last ascending, inside [0, limit].
 bool ranges_ok(const int32_t* dev, int32_t rows, int width, int32_t limit) {
@@ -91,6 +94,7 @@ uattn_status check_logits(const uattn::LogitsLaunch& a) {
     return UATTN_EINVAL;
   if (a.mask != nullptr && a.mask_stride < (static_cast<int64_t>(a.vocab) + 31) / 32) return UATTN_EINVAL;
   if (a.mask != nullptr && a.mask_rows == nullptr && a.num_masks < a.num_rows) return UATTN_EINVAL;
+  if (a.num_tokens > kMaxListed || a.num_bias > kMaxListed) return UATTN_EUNSUPPORTED;
   if (a.num_rows == 0) return UATTN_OK;
   if (!a.logits || !a.out || !aligned16(a.logits) || !aligned16(a.out)) return UATTN_EINVAL;
   if (validate_env()) {
@@ -591,6 +595,7 @@ uattn_status uattn_embedding(const int32_t* ids, const void* table, int64_t tabl
   if (num_tokens < 0 || vocab <= 0 || hidden_dim <= 0 || (hidden_dim % 8) != 0 || !is_finite(scale)) return UATTN_EINVAL;
   if (table_stride < hidden_dim || out_stride < hidden_dim || (table_stride % 8) != 0 || (out_stride % 8) != 0)
     return UATTN_EINVAL;
+  if (hidden_dim > kMaxEmbeddingWidth) return UATTN_EUNSUPPORTED;
   if (num_tokens == 0) return UATTN_OK;
   if (!ids || !table || !out || !aligned16(table) || !aligned16(out)) return UATTN_EINVAL;
   if (validate_env() && !all_below(ids, num_tokens, vocab)) return UATTN_EINVAL;
@@ -608,7 +613,7 @@ uattn_status uattn_embedding(const int32_t* ids, const void* table, int64_t tabl
 }
 
 size_t uattn_embedding_backward_workspace_bytes(int32_t num_tokens, int32_t hidden_dim) {
-  if (num_tokens <= 0 || hidden_dim <= 0 || num_tokens > kMaxSortedTokens) return 0;
+  if (num_tokens <= 0 || hidden_dim <= 0 || num_tokens > kMaxSortedTokens || hidden_dim > kMaxEmbeddingWidth) return 0;
   return uattn::embedding_backward_ws_bytes(num_tokens, hidden_dim);
 }
 
@@ -620,7 +625,7 @@ uattn_status uattn_embedding_backward(const void* dout, int64_t dout_stride, con
   if ((grad_fp32 & ~1) != 0 || (accumulate & ~1) != 0) return UATTN_EINVAL;
   if (grad_stride < hidden_dim || (grad_stride % (grad_fp32 ? 4 : 8)) != 0) return UATTN_EINVAL;
   if (dout_stride < hidden_dim || (dout_stride % 8) != 0) return UATTN_EINVAL;
-  if (num_tokens > kMaxSortedTokens) return UATTN_EUNSUPPORTED;
+  if (num_tokens > kMaxSortedTokens || hidden_dim > kMaxEmbeddingWidth) return UATTN_EUNSUPPORTED;
   if (num_tokens == 0 && accumulate) return UATTN_OK;
   if (!grad || !aligned16(grad)) return UATTN_EINVAL;
   if (num_tokens > 0 && (!dout || !ids || !aligned16(dout))) return UATTN_EINVAL;

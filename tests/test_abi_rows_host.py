@@ -54,7 +54,7 @@ def test_residual_norm_backward(lib, kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(T=-1), 1), (dict(V=0), 1), (dict(H=0), 1), (dict(H=12), 1), (dict(scale=NAN), 1), (dict(ts=60), 1), (dict(ts=68), 1),
     (dict(os=32), 1), (dict(ids=None), 1), (dict(table=None), 1), (dict(out=None), 1), (dict(table=P(24)), 1),
-    (dict(out=P(24)), 1), (dict(T=0), 0),
+    (dict(out=P(24)), 1), (dict(T=0), 0), (dict(H=(1 << 20) + 8, ts=1 << 21, os=1 << 21), 2),
 ])
 def test_embedding(lib, kw, code):
     d = dict(ids=P(16), table=P(16), ts=64, scale=1.0, T=4, V=10, H=64, out=P(16), os=64, stream=None)
@@ -66,6 +66,7 @@ def test_embedding(lib, kw, code):
     (dict(gs=60), 1), (dict(gs=66), 1), (dict(gs=68, fp32=0), 1), (dict(fp32=2), 1), (dict(acc=-1), 1), (dict(grad=None), 1),
     (dict(dout=None), 1), (dict(ids=None), 1), (dict(dout=P(24)), 1), (dict(grad=P(24)), 1), (dict(T=(1 << 30) + 1), 2),
     (dict(ws=None), 3), (dict(wsb=100), 3), (dict(ws=P(24)), 3), (dict(T=0, acc=1), 0),
+    (dict(H=(1 << 20) + 8, ds=1 << 21, gs=1 << 21), 2),
 ])
 def test_embedding_backward(lib, kw, code):
     d = dict(dout=P(16), ds=64, ids=P(16), scale=1.0, T=4, V=10, H=64, grad=P(16), gs=64, fp32=1, acc=0, ws=P(16), wsb=1 << 20,
@@ -77,11 +78,11 @@ LOGITS = [
     (dict(T=-1), 1), (dict(V=0), 1), (dict(ls=96), 1), (dict(ls=108), 1), (dict(os=96), 1), (dict(os=108), 1),
     (dict(N=-1), 1), (dict(tok=None), 1), (dict(hist=None), 1), (dict(pen=None), 1), (dict(K=-1), 1), (dict(ms=3), 1),
     (dict(mr=None), 1), (dict(z=None), 1), (dict(out=None), 1), (dict(z=P(24)), 1), (dict(out=P(24)), 1), (dict(T=0), 0),
-    (dict(T=0, z=None, out=None), 0),
+    (dict(T=0, z=None, out=None), 0), (dict(N=(1 << 30) + 1), 2),
 ]
 
 
-@pytest.mark.parametrize("kw,code", LOGITS + [(dict(M=-1), 1), (dict(bi=None), 1), (dict(bv=None), 1)])
+@pytest.mark.parametrize("kw,code", LOGITS + [(dict(M=-1), 1), (dict(bi=None), 1), (dict(bv=None), 1), (dict(M=(1 << 30) + 1), 2)])
 def test_logits_process(lib, kw, code):
     d = dict(z=P(16), ls=104, T=4, V=100, tok=P(16), N=9, hist=P(16), pen=P(16), bi=P(16), bv=P(16), M=2, br=P(16), mask=P(16),
              ms=4, K=2, mr=P(16), out=P(16), os=104, stream=None)
@@ -109,7 +110,7 @@ def test_workspace_bytes(lib):
     from paper_2609_35140_amd import uattn
     f, g = uattn.residual_norm_backward_workspace_bytes, uattn.embedding_backward_workspace_bytes
     assert f(0, 64) == f(-1, 64) == f(4, 12) == f(4, 1 << 20) == 0
-    assert g(0, 64) == g(-1, 64) == g(4, 0) == 0
+    assert g(0, 64) == g(-1, 64) == g(4, 0) == g(4, (1 << 20) + 8) == 0
     # three sums of a group of rows each; they stop growing with the tokens
     assert f(1, 64) == 3 * 64 * 4 and f(100000, 4096) == f(1 << 30, 4096)
     # sorted keys and order, and for every 32 tokens two fp32 rows of partial sums

@@ -194,6 +194,21 @@ def test_rows_past_2_31_elements(ua):
     assert not table[:V - 3].any()
 
 
+@pytest.mark.parametrize("fp32", [True, False])
+def test_widest_rows(ua, fp32):
+    """The most columns there may be, small whole numbers: sums up to 70 * 3 are exact in fp32 and in bf16."""
+    import torch
+    T, V, H = 70, 3, 1 << 20
+    ids = gu.dev_i32(inputs.rng(356, T).integers(-1, V, T).astype(np.int32))
+    table = torch.arange(V * H, device="cuda").remainder(7).sub(3).to(torch.bfloat16).reshape(V, H)
+    out = ua.embedding(ids, table)
+    for t in range(T):
+        assert torch.equal(out[t], table[ids[t]] if ids[t] >= 0 else torch.zeros_like(out[t]))
+    grad = ua.embedding_backward(out, ids, V, dtype=torch.float32 if fp32 else torch.bfloat16)
+    want = torch.stack([table[v].float() * int((ids == v).sum()) for v in range(V)])
+    assert torch.equal(grad.float(), want if fp32 else want.to(torch.bfloat16).float())
+
+
 def test_validation(ua, monkeypatch):
     import torch
     monkeypatch.setenv("UATTN_VALIDATE", "1")
