@@ -534,6 +534,8 @@ def _elsewhere(device: int, stream):
         return None if device == torch._C._cuda_getDevice() else torch.cuda.device(device)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
+    if stream.device_index != device:
+        raise ValueError(f"stream is of GPU {stream.device_index}, the tensors are on GPU {device}")
     return torch.cuda.stream(stream)
 
 

@@ -116,3 +116,14 @@ def test_workspace_bytes(lib):
     # sorted keys and order, and for every 32 tokens two fp32 rows of partial sums
     assert 16 * 4096 + 2 * 128 * 1024 * 4 <= g(4096, 1024) <= 64 * 4096 + 2 * 128 * 1024 * 4 + (1 << 20)
     assert g(1 << 30, 8) > 1 << 32
+
+
+def test_stream_of_another_gpu_is_refused():
+    """The binding moves to the tensors' GPU, so a call for such a stream would run on another one than it names."""
+    from paper_2609_35140_amd import uattn
+
+    class Stream:
+        cuda_stream, device_index = 5, 1
+
+    with pytest.raises(ValueError, match="GPU 1"):
+        uattn._elsewhere(0, Stream())
