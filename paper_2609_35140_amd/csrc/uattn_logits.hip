@@ -8,7 +8,7 @@
 // in fp32 (the division as a product with 1 / repetition), rounded to bf16 once.
 //
 // A workgroup takes one stretch of up to 8192 entries (the vocabulary in equal parts,
-// sixteen entries to a thread) of up to kMaxRows consecutive rows.  It counts the
+// sixteen entries to a thread) of some consecutive rows.  It counts the
 // history's tokens that fall into the stretch in LDS (whole numbers, so the order of
 // the atomics does not show) and streams the stretch.  Rows of an update are
 // successive prefixes of a sequence: where a row's history is the one before it and
@@ -27,7 +27,10 @@ constexpr int kLogitsThreads = 512;  // at most
 constexpr int kLogitsVecs = 2;
 constexpr int kThreadEntries = 8 * kLogitsVecs;
 constexpr int kMostEntries = kLogitsThreads * kThreadEntries;  // of a stretch
-constexpr int kMaxRows = 16;
+// Rows to a workgroup where there are many: few, as the rows in flight then lie close together (8000 rows of
+// 151,936 with 2000 tokens of history: 820 us with 3, 910 with 5, 990 with 16), or four times as many where a
+// long history would be counted for each three (3200 rows, 31,000 tokens: 498 us with 3, 430 with 5, 396 with 7).
+constexpr int kFewRows = 3, kParts = 3, kLongHistory = 24;  // tokens to a thread
 constexpr uint32_t kPrompt = 0x80000000u;  // of a count: the entry occurs in the prompt
 constexpr int32_t kNoBias = INT32_MIN;     // of the bias table: as a float, -0, which changes no sum
 
@@ -44,9 +47,11 @@ struct LogitsParams {
   const uint32_t* mask;      // [num_masks][mask_stride]
   const int32_t* mask_rows;  // [rows], or null: row t has mask t
   int64_t in_stride, logits_stride, out_stride, mask_stride;
-  int32_t num_rows, vocab, num_tokens, num_bias, num_masks, stretches;
+  int32_t num_rows, vocab, num_tokens, num_bias, num_masks;
+  uint32_t stretches;
   bool stream;    // the output past the caches
-  int32_t rows;   // consecutive rows to a workgroup
+  int32_t rows;   // consecutive rows to a workgroup, or `parts` times as many
+  int32_t parts;  // 1 or kParts
   int32_t first;  // workgroups of the launches before this one
 };
 
@@ -57,15 +62,15 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
 }
 
 template <bool kGrad, bool kBias>
-__global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(LogitsParams p) {
+__global__ __launch_bounds__(kLogitsThreads, 6) void logits_kernel(LogitsParams p) {
   // counts, and behind them the biases (in their place where the counts serve one row alone)
   extern __shared__ __align__(16) uint32_t table[];
   int32_t* bias_table = reinterpret_cast<int32_t*>(table) + (p.rows > 1 ? blockDim.x * kThreadEntries : 0);
   const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x, stretch = threads * kThreadEntries;
-  const int64_t unit = p.first + static_cast<int64_t>(blockIdx.x);
-  const int64_t row0 = unit / p.stretches * p.rows;
-  const int v0 = static_cast<int>(unit % p.stretches) * stretch, n = min(stretch, p.vocab - v0);
-  const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows), p.num_rows - row0));
+  const uint32_t unit = p.first + blockIdx.x, group = unit / p.stretches, part = p.parts > 1 ? group % kParts : 0;
+  const int64_t row0 = static_cast<int64_t>(group - part) * p.rows;
+  const int v0 = static_cast<int>(unit - group * p.stretches) * stretch, n = min(stretch, p.vocab - v0);
+  const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows) * p.parts, p.num_rows - row0));
 
   // Lane r of every wave keeps row r's arguments; the loops below read them from there.
   int begin = 0, split = 0, end = 0, bias_begin = 0, bias_end = 0, mask_row = -1;
@@ -99,11 +104,25 @@ __global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(L
   }
   const int last_token = lane < rows && from >= 0 && end == from + 1 ? p.tokens[from] : -1;
   const bool one_here = static_cast<uint32_t>(last_token) - v0 < static_cast<uint32_t>(n);
+  // the workgroup's rows: its part of the `rows`, or all of them to the first where they share a long history
+  const int first_row = part * p.rows;
+  int last_row = min(first_row + p.rows, rows);
+  if (p.parts > 1 && lane_int(end, 0) - lane_int(begin, 0) > kLongHistory * threads && __ballot(lane > 0 && lane < rows && from < 0) == 0) {
+    if (first_row > 0) return;
+    last_row = rows;
+  }
   const bool active = begin < end && (rep != 1.f || freq != 0.f || pres != 0.f);
-  const uint64_t actives = __ballot(active);
+  const uint64_t actives = __ballot(active && lane >= first_row && lane < last_row);
   const int bias_before = __shfl_up(bias_begin, 1, 64), bias_until = __shfl_up(bias_end, 1, 64);
-  const bool new_bias = lane == 0 || bias_before != bias_begin || bias_until != bias_end;
+  const bool new_bias = lane == first_row || bias_before != bias_begin || bias_until != bias_end;
 
+  // a stretch's last piece, where it is shorter than others: its bounds are the workgroup's, not a thread's
+  const int whole = n & ~7, rest = n & 7;
+  auto load_rest = [&](const uint16_t* in) {
+    u32x4 q = {0, 0, 0, 0};
+    for (int e = 0; e < rest; ++e) q[e / 2] |= static_cast<uint32_t>(in[whole + e]) << (16 * (e & 1));
+    return q;
+  };
   auto load = [&](int r, u32x4 (&w)[kLogitsVecs], uint32_t (&keep)[kLogitsVecs]) {
     const uint16_t* in = p.in + (row0 + r) * p.in_stride + v0;
     const int m = lane_int(mask_row, r);
@@ -113,10 +132,10 @@ __global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(L
       const int piece = tid + i * threads, e0 = 8 * piece;
       w[i] = u32x4{0, 0, 0, 0};
       keep[i] = 0xFF;
-      if (e0 + 8 <= n)
+      if (e0 < whole)
         w[i] = load16(in, 0, piece);
-      else
-        for (int e = 0; e < n - e0; ++e) w[i][e / 2] |= static_cast<uint32_t>(in[e0 + e]) << (16 * (e & 1));
+      else if (e0 < n)
+        w[i] = load_rest(in);
       if (m >= 0 && e0 < n) keep[i] = mask[piece];
     }
   };
@@ -140,23 +159,18 @@ __global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(L
 
   // Backward: the logits of the pieces that hold entries of the history, and which of the next row's are here already
   // (those that this row's counts ask for; a row's own new ones are read when its counts are known).
-  u32x4 next_z[kLogitsVecs];
+  u32x4 z[kLogitsVecs];
   bool have_z[kLogitsVecs] = {};
   auto load_z = [&](int r, int i) {
     const int piece = tid + i * threads;
-    const uint16_t* z = p.logits + (row0 + r) * p.logits_stride + v0;
-    u32x4 q = {0, 0, 0, 0};
-    if (8 * piece + 8 <= n)
-      q = load16(z, 0, piece);
-    else
-      for (int e = 0; e < n - 8 * piece; ++e) q[e / 2] |= static_cast<uint32_t>(z[8 * piece + e]) << (16 * (e & 1));
-    return q;
+    const uint16_t* in = p.logits + (row0 + r) * p.logits_stride + v0;
+    return 8 * piece < whole ? load16(in, 0, piece) : load_rest(in);
   };
 
   u32x4 next[kLogitsVecs];
   uint32_t next_keep[kLogitsVecs];
-  load(0, next, next_keep);
-  for (int r = 0; r < rows; ++r) {
+  load(first_row, next, next_keep);
+  for (int r = first_row; r < last_row; ++r) {
     u32x4 w[kLogitsVecs];
     uint32_t keep[kLogitsVecs];
 #pragma unroll
@@ -170,9 +184,10 @@ __global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(L
       const int i = lane_int(bias_begin, r) + tid;
       if (i < lane_int(bias_end, r)) first_id = p.bias_ids[i];
     }
-    if (r + 1 < rows) load(r + 1, next, next_keep);
+    if (r + 1 < last_row) load(r + 1, next, next_keep);
     if (actives != 0) {
-      const int lo = lane_int(begin, r), hi = lane_int(end, r), response = lane_int(split, r), at = lane_int(from, r);
+      const int lo = lane_int(begin, r), hi = lane_int(end, r), response = lane_int(split, r);
+      const int at = r > first_row ? lane_int(from, r) : -1;
       if (at < 0) {
         __syncthreads();
 #pragma unroll
@@ -186,60 +201,88 @@ __global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(L
         __syncthreads();
       }
     }
+    auto counts = [&](int i, uint32_t (&seen)[8]) {
+      const u32x4* t = reinterpret_cast<const u32x4*>(table) + 2 * (tid + i * threads);
+      const u32x4 a = t[0], b = t[1];
+      uint32_t any = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        seen[e] = a[e];
+        seen[e + 4] = b[e];
+        any |= a[e] | b[e];
+      }
+      return any != 0;
+    };
+    auto put = [&](int i, float (&x)[8]) {
+      uint16_t* out = p.out + (row0 + r) * p.out_stride + v0;
+      const bool masked = lane_int(mask_row, r) >= 0;
+      const int piece = tid + i * threads, e0 = 8 * piece;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = keep[i] >> e & 1 ? x[e] : (kGrad ? 0.f : -__builtin_inff());
+      }
+      const u32x4 o = pack8(x);
+      if (e0 < whole)
+        store16_as(p.stream, out, 0, piece, o);
+      else
+        for (int e = 0; e < rest; ++e) out[whole + e] = static_cast<uint16_t>(o[e / 2] >> (16 * (e & 1)));
+    };
+    if constexpr (kGrad) {
+      const float mul = lane_float(rep, r), inv = 1.f / mul;
+      uint32_t hits[kLogitsVecs] = {};  // bit e: the piece's entry e is in the history; bit 8 + e: and its logit is above 0
+      if (actives >> r & 1) {
+#pragma unroll
+        for (int i = 0; i < kLogitsVecs; ++i) {
+          uint32_t seen[8];
+          counts(i, seen);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) hits[i] |= seen[e] != 0 ? 1u << e : 0;
+          if (hits[i] != 0 && !have_z[i]) z[i] = load_z(r, i);
+        }
+#pragma unroll
+        for (int i = 0; i < kLogitsVecs; ++i) {
+          if (hits[i] == 0) continue;
+          float zs[8];
+          unpack8(z[i], zs);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) hits[i] |= zs[e] > 0.f ? 256u << e : 0;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kLogitsVecs; ++i) {
+        have_z[i] = hits[i] != 0 && r + 1 < last_row;
+        if (have_z[i]) z[i] = load_z(r + 1, i);
+      }
+#pragma unroll
+      for (int i = 0; i < kLogitsVecs; ++i) {
+        if (8 * (tid + i * threads) >= n) break;
+        float x[8];
+        unpack8(w[i], x);
+        if (hits[i] != 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = hits[i] >> e & 1 ? x[e] * (hits[i] >> (8 + e) & 1 ? inv : mul) : x[e];
+        }
+        put(i, x);
+      }
+      continue;
+    }
     float x[kLogitsVecs][8];
 #pragma unroll
     for (int i = 0; i < kLogitsVecs; ++i) unpack8(w[i], x[i]);
     if (actives >> r & 1) {
       const float mul = lane_float(rep, r), inv = 1.f / mul, f = lane_float(freq, r), q = lane_float(pres, r);
-      auto counts = [&](int i, uint32_t (&seen)[8]) {
-        const u32x4* t = reinterpret_cast<const u32x4*>(table) + 2 * (tid + i * threads);
-        const u32x4 a = t[0], b = t[1];
-        uint32_t any = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          seen[e] = a[e];
-          seen[e + 4] = b[e];
-          any |= a[e] | b[e];
-        }
-        return any != 0;
-      };
-      if constexpr (kGrad) {
-        uint32_t seen[kLogitsVecs][8];
-        u32x4 z[kLogitsVecs];
+      for (int i = 0; i < kLogitsVecs; ++i) {
+        uint32_t seen[8];
+        if (!counts(i, seen)) continue;
 #pragma unroll
-        for (int i = 0; i < kLogitsVecs; ++i) {
-          const bool hit = counts(i, seen[i]);
-          z[i] = next_z[i];
-          if (hit && !have_z[i]) z[i] = load_z(r, i);
-          have_z[i] = hit && r + 1 < rows;
-        }
-#pragma unroll
-        for (int i = 0; i < kLogitsVecs; ++i)
-          if (have_z[i]) next_z[i] = load_z(r + 1, i);
-#pragma unroll
-        for (int i = 0; i < kLogitsVecs; ++i) {
-          float zs[8];
-          unpack8(z[i], zs);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[i][e] = seen[i][e] == 0 ? x[i][e] : x[i][e] * (zs[e] > 0.f ? inv : mul);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kLogitsVecs; ++i) {
-          uint32_t seen[8];
-          if (!counts(i, seen)) continue;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t times = seen[e] & ~kPrompt;
-            float y = x[i][e] * (x[i][e] > 0.f ? inv : mul);
-            y = __builtin_fmaf(-f, static_cast<float>(times), y) - (times != 0 ? q : 0.f);
-            x[i][e] = seen[e] == 0 ? x[i][e] : y;
-          }
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t times = seen[e] & ~kPrompt;
+          float y = x[i][e] * (x[i][e] > 0.f ? inv : mul);
+          y = __builtin_fmaf(-f, static_cast<float>(times), y) - (times != 0 ? q : 0.f);
+          x[i][e] = seen[e] == 0 ? x[i][e] : y;
         }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLogitsVecs; ++i) have_z[i] = false;
     }
     if (kBias && lane_int(new_bias, r) != 0) {
       const int lo = lane_int(bias_begin, r), hi = lane_int(bias_end, r);
@@ -279,21 +322,10 @@ __global__ __launch_bounds__(kLogitsThreads, kGrad ? 4 : 6) void logits_kernel(L
         for (int e = 0; e < 8; ++e) x[i][e] = x[i][e] + add[e];
       }
     }
-    uint16_t* out = p.out + (row0 + r) * p.out_stride + v0;
-    const bool masked = lane_int(mask_row, r) >= 0;
 #pragma unroll
     for (int i = 0; i < kLogitsVecs; ++i) {
-      const int piece = tid + i * threads, e0 = 8 * piece;
-      if (e0 >= n) break;
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = keep[i] >> e & 1 ? x[i][e] : (kGrad ? 0.f : -__builtin_inff());
-      }
-      const u32x4 o = pack8(x[i]);
-      if (e0 + 8 <= n)
-        store16_as(p.stream, out, 0, piece, o);
-      else
-        for (int e = 0; e < n - e0; ++e) out[e0 + e] = static_cast<uint16_t>(o[e / 2] >> (16 * (e & 1)));
+      if (8 * (tid + i * threads) >= n) break;
+      put(i, x[i]);
     }
   }
 }
@@ -323,9 +355,10 @@ hipError_t launch_logits(const LogitsLaunch& a, bool grad, hipStream_t stream) {
   p.stretches = (a.vocab - 1) / kMostEntries + 1;
   const int threads = ((a.vocab - 1) / p.stretches / kThreadEntries / 64 + 1) * 64;  // equal parts, whole waves
   p.stream = streams(a.num_rows, a.vocab);
-  // few rows are spread over all CUs, many share their counts
+  // few rows are spread over all CUs, sixteen workgroups to each
   const int64_t share = static_cast<int64_t>(a.num_rows) * p.stretches / (16 * device_cus());
-  p.rows = static_cast<int>(share < 1 ? 1 : share > kMaxRows ? kMaxRows : share);
+  p.rows = static_cast<int>(share < 1 ? 1 : share > kFewRows ? kFewRows : share);
+  p.parts = share < kFewRows ? 1 : kParts;
   const int64_t groups = (static_cast<int64_t>(a.num_rows) + p.rows - 1) / p.rows;
   const size_t lds = sizeof(uint32_t) * threads * kThreadEntries * (a.bias_rows != nullptr && p.rows > 1 ? 2 : 1);
   return launch_parts(groups * p.stretches, threads, [&](int first, unsigned n) {

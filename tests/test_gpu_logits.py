@@ -198,6 +198,53 @@ def test_histories_that_go_on_from_row_to_row(ua, T, V):
         assert torch.equal(row.view(torch.int16), back[at].view(torch.int16)), t
 
 
+@pytest.mark.parametrize("T,V", [(9000, 33), (13000, 40), (13001, 1000), (5000, 16391)])
+def test_many_rows_share_their_counts(ua, T, V):
+    """So many rows that a workgroup takes several (and more of them where they share a long history), in sequences that
+    begin and end inside a group: what the same rows get in calls of too few rows for that."""
+    import torch
+    g = inputs.rng(357, T, V)
+    N = 30000
+    tok = np.minimum(np.exp(g.random(N) * np.log(V + 1)).astype(np.int64) - 1, V - 1)
+    hist, b, s, e = [], 0, 40, 3
+    for _ in range(T):
+        k = g.integers(0, 40)
+        if k == 0:
+            b = int(g.integers(0, 15000))
+            s = b + int(g.integers(0, 3000))
+            e = b + int(g.choice([0, 30, 1500, 1600, 9300, 14000]))
+        elif k == 1:
+            e = max(b, e - 5)
+        else:
+            e += int(g.choice([0, 1, 2], p=[0.1, 0.8, 0.1]))
+        hist.append((b, s, min(e, N)))
+    pen = np.stack([1 + g.random(T), g.random(T), g.random(T)], 1)
+    pen[g.random(T) < 0.1] = (1, 0, 0)
+    M = 500
+    bias_rows = np.sort(g.integers(0, M, ((T + 6) // 7, 2)), axis=1).repeat(7, axis=0)[:T]
+    tokens, ids, values = gu.dev_i32(tok), gu.dev_i32(g.integers(0, V, M)), _f32(g.standard_normal(M))
+    z = _rows(inputs.normal_bf16((T, V), 2.0, 358))[:, :V]
+    h, p, br = gu.dev_i32(hist), _f32(pen), gu.dev_i32(bias_rows)
+    mask, mr = gu.dev_i32(g.integers(-2 ** 31, 2 ** 31, (3, (V + 31) // 32))), gu.dev_i32(g.integers(-1, 3, T))
+    for bias in (False, True):
+        def run(at):
+            more = dict(bias_ids=ids, bias_values=values, bias_rows=br[at], mask=mask, mask_rows=mr[at]) if bias else {}
+            return ua.logits_process(z[at], tokens, h[at], p[at], **more)
+
+        full = run(slice(0, T))
+        for t in range(0, T, 1000):
+            at = slice(t, min(t + 1000, T))
+            assert torch.equal(run(at).view(torch.int16), full[at].view(torch.int16)), t
+
+    def back(at):
+        return ua.logits_process_backward(z[at], z[at], tokens, h[at], p[at], mask, mr[at])
+
+    full = back(slice(0, T))
+    for t in range(0, T, 1000):
+        at = slice(t, min(t + 1000, T))
+        assert torch.equal(back(at).view(torch.int16), full[at].view(torch.int16)), t
+
+
 def test_update_rows_equal_decode_rows(ua):
     """A packed sequence's rows in one call, and each as the decode step at its position processes it: the same bits, and
     the same log-probability."""
