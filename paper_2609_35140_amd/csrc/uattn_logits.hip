@@ -61,7 +61,9 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
 }
 
-template <bool kGrad, bool kBias>
+// kOnce: the input passes the caches by, which serve the logits beside it (backward, us: 334 MB of gradient 148 -> 140,
+// 48 MB 32 -> 30; 32 MB that the caches still hold 19.5 -> 21).
+template <bool kGrad, bool kBias, bool kOnce>
 __global__ __launch_bounds__(kLogitsThreads, 6) void logits_kernel(LogitsParams p) {
   // counts, and behind them the biases (in their place where the counts serve one row alone)
   extern __shared__ __align__(16) uint32_t table[];
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(kLogitsThreads, 6) void logits_kernel(LogitsParams 
       w[i] = u32x4{0, 0, 0, 0};
       keep[i] = 0xFF;
       if (e0 < whole)
-        w[i] = load16(in, 0, piece);
+        w[i] = kOnce ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(in) + piece) : load16(in, 0, piece);
       else if (e0 < n)
         w[i] = load_rest(in);
       if (m >= 0 && e0 < n) keep[i] = mask[piece];
@@ -363,12 +365,14 @@ hipError_t launch_logits(const LogitsLaunch& a, bool grad, hipStream_t stream) {
   const size_t lds = sizeof(uint32_t) * threads * kThreadEntries * (a.bias_rows != nullptr && p.rows > 1 ? 2 : 1);
   return launch_parts(groups * p.stretches, threads, [&](int first, unsigned n) {
     p.first = first;
-    if (grad)
-      hipLaunchKernelGGL((logits_kernel<true, false>), dim3(n), dim3(threads), lds, stream, p);
+    if (grad && p.stream)
+      hipLaunchKernelGGL((logits_kernel<true, false, true>), dim3(n), dim3(threads), lds, stream, p);
+    else if (grad)
+      hipLaunchKernelGGL((logits_kernel<true, false, false>), dim3(n), dim3(threads), lds, stream, p);
     else if (a.bias_rows != nullptr)
-      hipLaunchKernelGGL((logits_kernel<false, true>), dim3(n), dim3(threads), lds, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, true, false>), dim3(n), dim3(threads), lds, stream, p);
     else
-      hipLaunchKernelGGL((logits_kernel<false, false>), dim3(n), dim3(threads), lds, stream, p);
+      hipLaunchKernelGGL((logits_kernel<false, false, false>), dim3(n), dim3(threads), lds, stream, p);
   });
 }
 
