@@ -549,7 +549,10 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t row, int
 // A wave to a piece and 512 columns, eight of the piece's rows in flight, added in order; the next piece's
 // record comes meanwhile.  Pieces differ in length, so a CU gets 32 workgroups one after another, not all
 // of its work at once (16,384 tokens, 32,000 x 4096 bf16: 116 us with 8 to a CU, 110 with 32, 113 with 128).
-template <bool kFp32, bool kAdd>
+// kOnce: the tokens' rows pass the caches by, which then take the sums (us for dout of 33 MB and a table of 131 57 -> 42, of
+// 131 and 262 103 -> 87; where the caches hold both, of 51 and 16 57 -> 61, of 4-16 and 65 21 -> 22.5; added to a table, of
+// which the sums' rows alone are touched, 134 MB 61 -> 67, 537 MB 285 -> 256).
+template <bool kFp32, bool kAdd, bool kOnce>
 __global__ __launch_bounds__(256, 6) void sum_pieces_kernel(GradParams p) {
   constexpr int kAhead = 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -575,7 +578,7 @@ __global__ __launch_bounds__(256, 6) void sum_pieces_kernel(GradParams p) {
         w[j] = u32x4{0, 0, 0, 0};
         if (j0 + j >= n) continue;
         const int64_t t = __builtin_amdgcn_readlane(mine, j0 + j);
-        if (here) w[j] = load16(p.dout, t * (p.dout_stride / 8), col / 8);
+        if (here) w[j] = load16_as<kOnce>(p.dout, t * (p.dout_stride / 8), col / 8);
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -780,9 +783,14 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   const int64_t units = static_cast<int64_t>(a.num_tokens) * ((a.hidden_dim + 511) / 512);
   const int64_t sum_grid = (units + 3) / 4 < 32 * cus ? (units + 3) / 4 : 32 * cus;
   const int64_t join_grid = units / kPiece + 1 < 4 * cus ? units / kPiece + 1 : 4 * cus;
+  const int64_t read = 2 * static_cast<int64_t>(a.num_tokens) * a.hidden_dim, table = static_cast<int64_t>(a.vocab) * a.hidden_dim * size;
+  const bool once = a.accumulate ? read >= int64_t{256} << 20 : read >= int64_t{24} << 20 && read + table >= int64_t{128} << 20;
   auto sums = [&](auto fp32, auto add) {
     constexpr bool kFp32 = decltype(fp32)::value, kAdd = decltype(add)::value;
-    hipLaunchKernelGGL((sum_pieces_kernel<kFp32, kAdd>), dim3(sum_grid), dim3(256), 0, stream, p);
+    if (once)
+      hipLaunchKernelGGL((sum_pieces_kernel<kFp32, kAdd, true>), dim3(sum_grid), dim3(256), 0, stream, p);
+    else
+      hipLaunchKernelGGL((sum_pieces_kernel<kFp32, kAdd, false>), dim3(sum_grid), dim3(256), 0, stream, p);
     if (a.num_tokens > kPiece)
       hipLaunchKernelGGL((join_pieces_kernel<kFp32, kAdd>), dim3(join_grid), dim3(64 * kJoinWaves), 0, stream, p);
   };

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kLogitsThreads, 6) void logits_kernel(LogitsParams 
       w[i] = u32x4{0, 0, 0, 0};
       keep[i] = 0xFF;
       if (e0 < whole)
-        w[i] = kOnce ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(in) + piece) : load16(in, 0, piece);
+        w[i] = load16_as<kOnce>(in, 0, piece);
       else if (e0 < n)
         w[i] = load_rest(in);
       if (m >= 0 && e0 < n) keep[i] = mask[piece];

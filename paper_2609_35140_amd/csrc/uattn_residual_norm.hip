@@ -23,7 +23,6 @@ struct NormParams {
   int64_t gate_stride;
   float scale, eps, inv_hidden;
   int32_t num_tokens, hidden;
-  bool stream;    // the outputs past the caches
   int32_t first;  // rows of the launches before this one
 };
 
@@ -34,7 +33,9 @@ __device__ __forceinline__ float inverse_rms(float mean, float eps) { return 1.0
 template <int kRowWaves>
 constexpr int kNormWaves = kRowWaves > 4 ? kRowWaves : 4;
 
-template <int kRowWaves, int kVecs>
+// kOnce: the rows pass the caches by, read and written (us: 39,855 x 1024 57 -> 54 with the reads, 8191 x 4096 50 -> 47; but
+// 2000 x 4096, which the caches hold, 12.1 -> 12.6).
+template <int kRowWaves, int kVecs, bool kOnce>
 __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kernel(NormParams p) {
   constexpr int kWaves = kNormWaves<kRowWaves>, kRows = kWaves / kRowWaves;
   __shared__ float slots[2][kWaves];
@@ -50,8 +51,8 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
   for (int i = 0; i < kVecs; ++i) {
     hw[i] = xw[i] = zero;
     if (!here || piece(i) >= pieces) continue;
-    hw[i] = load16(p.residual, base, piece(i));
-    if (p.x != nullptr) xw[i] = load16(p.x, base, piece(i));
+    hw[i] = load16_as<kOnce>(p.residual, base, piece(i));
+    if (p.x != nullptr) xw[i] = load16_as<kOnce>(p.x, base, piece(i));
   }
   float s[kVecs][8];
 #pragma unroll
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[i][e] = __builtin_fmaf(p.scale, u[e], s[i][e]);
-      store16_as(p.stream, p.residual_out, base, piece(i), pack8(s[i]));
+      store16_as(kOnce, p.residual_out, base, piece(i), pack8(s[i]));
     }
   }
   if (p.y == nullptr) return;
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
     unpack8(load16(p.pre, 0, piece(i)), g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) g[e] = s[i][e] * r * g[e];
-    store16_as(p.stream, p.y, base, piece(i), pack8(g));
+    store16_as(kOnce, p.y, base, piece(i), pack8(g));
   }
 }
 
@@ -422,13 +423,17 @@ int norm_sets(int64_t num_tokens, int64_t hidden_dim) {
 
 hipError_t launch_residual_norm(const ResidualNormLaunch& a, hipStream_t stream) {
   NormParams p{a.x, a.post_weight, a.gate, a.residual, a.pre_weight, a.residual_out, a.y, a.gate_stride, a.scale, a.eps,
-               1.0f / a.hidden_dim, a.num_tokens, a.hidden_dim, streams(a.num_tokens, a.hidden_dim), 0};
+               1.0f / a.hidden_dim, a.num_tokens, a.hidden_dim, 0};
+  const bool once = streams(a.num_tokens, a.hidden_dim);
   auto launch = [&](auto row_waves, auto vecs) {
     constexpr int kRowWaves = decltype(row_waves)::value, kVecs = decltype(vecs)::value;
     constexpr int kWaves = kNormWaves<kRowWaves>, kRows = kWaves / kRowWaves;
     return launch_parts((static_cast<int64_t>(a.num_tokens) + kRows - 1) / kRows, 64 * kWaves, [&](int first, unsigned n) {
       p.first = first * kRows;
-      hipLaunchKernelGGL((residual_norm_kernel<kRowWaves, kVecs>), dim3(n), dim3(64 * kWaves), 0, stream, p);
+      if (once)
+        hipLaunchKernelGGL((residual_norm_kernel<kRowWaves, kVecs, true>), dim3(n), dim3(64 * kWaves), 0, stream, p);
+      else
+        hipLaunchKernelGGL((residual_norm_kernel<kRowWaves, kVecs, false>), dim3(n), dim3(64 * kWaves), 0, stream, p);
     });
   };
   using std::integral_constant;

@@ -51,6 +51,13 @@ __device__ __forceinline__ void store16(void* base, int64_t uniform, uint32_t pi
   *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + 16 * uniform + 16u * piece) = w;
 }
 
+// A read that passes the caches by, or not.
+template <bool kOnce>
+__device__ __forceinline__ u32x4 load16_as(const void* base, int64_t uniform, uint32_t piece) {
+  const u32x4* from = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base) + 16 * uniform + 16u * piece);
+  if constexpr (kOnce) return __builtin_nontemporal_load(from);
+  return *from;
+}
 // Outputs past the caches or not.  (The empty asm keeps the two stores apart: merged, they would both be plain.)
 __device__ __forceinline__ void store16_as(bool stream, void* base, int64_t uniform, uint32_t piece, const u32x4& w) {
   u32x4* to = reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + 16 * uniform + 16u * piece);
