@@ -539,6 +539,13 @@ def _elsewhere(device: int, stream):
     return torch.cuda.stream(stream)
 
 
+def _stream_on(device: int) -> int:
+    """The handle of the device's current stream."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 def _gpu_of(t, name) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
@@ -626,7 +633,7 @@ def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None
         else:
             _whole(y, bf16, shape, dev, "y")
     _check(_load().uattn_residual_norm(_ptr(x), _ptr(post_weight), _ptr(gate), gate_stride, scale, residual.data_ptr(),
-                                       _ptr(pre_weight), eps, T, H, _ptr(residual_out), _ptr(y), _stream(None)))
+                                       _ptr(pre_weight), eps, T, H, _ptr(residual_out), _ptr(y), _stream_on(dev)))
     return (residual if x is None else residual_out), y
 
 
@@ -698,7 +705,7 @@ def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=N
     _check(_load().uattn_residual_norm_backward(
         _ptr(dy), _ptr(dresidual_out), residual_out.data_ptr(), _ptr(pre_weight), _ptr(x), _ptr(post_weight), _ptr(gate),
         gate_stride, scale, eps, T, H, dresidual.data_ptr(), _ptr(dx), _ptr(d[0]), _ptr(d[1]), _ptr(d[2]),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(None)))
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_on(dev)))
     return dresidual, dx, d[0], d[1], d[2]
 
 
@@ -719,7 +726,7 @@ def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
     T, (V, H) = ids.shape[0], table.shape
     out = _out_rows(out, table, T, H)
     _check(_load().uattn_embedding(ids.data_ptr(), table.data_ptr(), _row_stride(table), scale, T, V, H, out.data_ptr(),
-                                   _row_stride(out), _stream(None)))
+                                   _row_stride(out), _stream_on(dev)))
     return out
 
 
@@ -763,7 +770,7 @@ def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, acc
     _check(_load().uattn_embedding_backward(
         dout.data_ptr(), _row_stride(dout), ids.data_ptr(), scale, T, vocab, H, grad.data_ptr(), _row_stride(grad),
         int(dtype == torch.float32), int(bool(accumulate)), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(None)))
+        workspace.numel() * workspace.element_size(), _stream_on(dev)))
     return grad
 
 
@@ -832,7 +839,7 @@ def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=N
     _check(_load().uattn_logits_process(
         logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens, _ptr(history), _ptr(penalties),
         _ptr(bias_ids), _ptr(bias_values), num_bias, _ptr(bias_rows), _ptr(mask), mask_stride, num_masks,
-        _ptr(mask_rows), out.data_ptr(), _row_stride(out), _stream(None)))
+        _ptr(mask_rows), out.data_ptr(), _row_stride(out), _stream_on(dev)))
     return out
 
 
@@ -859,7 +866,7 @@ def logits_process_backward(dout, logits, tokens=None, history=None, penalties=N
     _check(_load().uattn_logits_process_backward(
         dout.data_ptr(), _row_stride(dout), logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens,
         _ptr(history), _ptr(penalties), _ptr(mask), mask_stride, num_masks, _ptr(mask_rows), out.data_ptr(),
-        _row_stride(out), _stream(None)))
+        _row_stride(out), _stream_on(dev)))
     return out
 
 
@@ -881,7 +888,7 @@ def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=N
     _whole(dlogp, torch.float32, (T,), dev, "dlogp")
     out = _out_rows(out, logits, T, V)
     _check(_load().uattn_logprob_backward(logits.data_ptr(), _row_stride(logits), targets.data_ptr(), dlogp.data_ptr(), T, V,
-                                          inv_temperature, out.data_ptr(), _row_stride(out), _stream(None)))
+                                          inv_temperature, out.data_ptr(), _row_stride(out), _stream_on(dev)))
     return out
 
 
