@@ -548,7 +548,7 @@ __device__ __forceinline__ void write_row(const GradParams& p, uint32_t row, int
 
 // A wave to a piece and 512 columns, eight of the piece's rows in flight, added in order; the next piece's
 // record comes meanwhile.  Pieces differ in length, so a CU gets 32 workgroups one after another, not all
-// of its work at once (16,384 tokens, 32,000 x 4096 bf16: 116 us with 8 to a CU, 110 with 32, 113 with 128).
+// of its work at once (16,384 tokens, 32,000 x 4096 bf16: 92 us with 8 to a CU, 87.6 with 32, 88.4 with 128).
 // kOnce: the tokens' rows pass the caches by, which then take the sums (us for dout of 33 MB and a table of 131 57 -> 42, of
 // 131 and 262 103 -> 87; where the caches hold both, of 51 and 16 57 -> 61, of 4-16 and 65 21 -> 22.5; added to a table, of
 // which the sums' rows alone are touched, 134 MB 61 -> 67, 537 MB 285 -> 256).
@@ -695,7 +695,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardLaunch& a, hipStream
   z.row_pieces = a.grad_stride * size / 16;
   z.pieces = static_cast<int32_t>(static_cast<int64_t>(a.hidden_dim) * size / 16);
   // workgroups of `threads` that write zeros: a row to a wave, in the order they start, so that neighbours are
-  // written together (151,936 x 4096 fp32: 482 us a call so, 514 with two to a CU that walk the table)
+  // written together (151,936 x 4096 fp32: 32 us less a call than with two to a CU that walk the table)
   auto zeroers = [&](int threads) {
     const int64_t waves = threads / 64, blocks = (z.end - z.begin + waves - 1) / waves;
     const int64_t most = static_cast<int64_t>(cus) * 131072 / threads;

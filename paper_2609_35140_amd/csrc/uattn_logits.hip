@@ -8,9 +8,9 @@
 // in fp32 (the division as a product with 1 / repetition), rounded to bf16 once.
 //
 // A workgroup takes one stretch of up to 8192 entries (the vocabulary in equal parts,
-// sixteen entries to a thread) of some consecutive rows.  It counts the
-// history's tokens that fall into the stretch in LDS (whole numbers, so the order of
-// the atomics does not show) and streams the stretch.  Rows of an update are
+// sixteen entries to a thread) of some consecutive rows.  It counts the history's
+// tokens that fall into the stretch in LDS (whole numbers, so the order of the
+// atomics does not show) and streams the stretch.  Rows of an update are
 // successive prefixes of a sequence: where a row's history is the one before it and
 // some more, only the new tokens are counted, and most of them fall into other
 // stretches.  Counts do not depend on how they came about, so a decode step's row and
@@ -28,9 +28,11 @@ constexpr int kLogitsVecs = 2;
 constexpr int kThreadEntries = 8 * kLogitsVecs;
 constexpr int kMostEntries = kLogitsThreads * kThreadEntries;  // of a stretch
 // Rows to a workgroup where there are many: few, as the rows in flight then lie close together (8000 rows of
-// 151,936 with 2000 tokens of history: 820 us with 3, 910 with 5, 990 with 16), or four times as many where a
-// long history would be counted for each three (3200 rows, 31,000 tokens: 498 us with 3, 430 with 5, 396 with 7).
-constexpr int kFewRows = 3, kParts = 3, kLongHistory = 24;  // tokens to a thread
+// 151,936 with 2000 tokens of history: 820 us with 3, 910 with 5, 990 with 16).  Where three rows share a history
+// that is long to count (so many tokens to a thread, or more), kParts times as many by the first of as many
+// workgroups (3200 rows with 31,000 tokens: 498 us with 3 rows, 408 so; 5000 entries, 30,000 tokens 278 and 222).
+// An odd number of parts, as workgroups go to the eight chiplets in turn.
+constexpr int kFewRows = 3, kParts = 3, kLongHistory = 24;
 constexpr uint32_t kPrompt = 0x80000000u;  // of a count: the entry occurs in the prompt
 constexpr int32_t kNoBias = INT32_MIN;     // of the bias table: as a float, -0, which changes no sum
 

@@ -46,7 +46,7 @@ __device__ __forceinline__ MaxSum combine(MaxSum a, MaxSum b, float k) {
 }
 
 // Bound by memory.  The row stays in registers between its sum and its gradient (kVecs 16-byte pieces to
-// a thread, all requested at once): it is read once and written once (4100 rows of 151,936: 488 us, 5.1 TB/s;
+// a thread, all requested at once): it is read once and written once (4100 rows of 151,936: 490 us, 5.1 TB/s;
 // read a second time from the caches it took 1755).  Pieces past kThreads * kVecs are read again.
 template <int kThreads, int kVecs>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradParams p) {
