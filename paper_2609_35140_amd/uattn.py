@@ -533,7 +533,9 @@ def _elsewhere(device: int, stream):
     if stream is None:
         return None if device == torch._C._cuda_getDevice() else torch.cuda.device(device)
     if not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
+        # 0 and 1 (hipStreamLegacy) are the default stream's handles; ExternalStream takes 0 for none and gives a stream of its own
+        handle = int(stream)
+        stream = torch.cuda.default_stream(device) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device=device)
     if stream.device_index != device:
         raise ValueError(f"stream is of GPU {stream.device_index}, the tensors are on GPU {device}")
     return torch.cuda.stream(stream)

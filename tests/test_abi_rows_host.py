@@ -127,3 +127,25 @@ def test_stream_of_another_gpu_is_refused():
 
     with pytest.raises(ValueError, match="GPU 1"):
         uattn._elsewhere(0, Stream())
+
+
+@pytest.mark.parametrize("handle", [0, 1])
+def test_handle_of_the_default_stream(monkeypatch, handle):
+    """0, and 1 by its other name, are the default stream's handles; torch would take 0 for no handle at all."""
+    import torch
+    from paper_2609_35140_amd import uattn
+
+    class Default:
+        cuda_stream = 0
+
+        def __init__(self, device):
+            self.device_index = device
+
+    def external(*args, **kw):
+        raise AssertionError("a handle of the default stream is no external stream")
+
+    monkeypatch.setattr(torch.cuda, "default_stream", Default)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", external)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: stream)
+    there = uattn._elsewhere(3, handle)
+    assert isinstance(there, Default) and there.device_index == 3
