@@ -141,6 +141,22 @@ def _need(cond: bool, msg: str):
         raise ValueError(msg)
 
 
+_MOST = 2 ** 31 - 1
+
+
+# ctypes drops what of a number does not fit the library's 32-bit sizes, so they are checked before.
+def _fits(*sizes) -> bool:
+    for n in sizes:
+        if not -_MOST <= n <= _MOST:
+            return False
+    return True
+
+
+def _sizes(*sizes):
+    if not _fits(*sizes):
+        raise ValueError(f"sizes are at most 2^31 - 1, got {max(sizes, key=abs)}")
+
+
 def _bf16_cuda(t, name):
     import torch
     if t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous():
@@ -182,6 +198,7 @@ def prefill(q, k, v, cu_seqlens, max_seqlen: int, softmax_scale: Optional[float]
     _need(k.shape == v.shape and k.shape[0] == T and k.shape[2] == d, "k/v shape mismatch")
     _need(cu_seqlens.dtype == torch.int32 and cu_seqlens.is_cuda and cu_seqlens.is_contiguous(),
           "cu_seqlens must be contiguous int32 on the GPU")
+    _sizes(T, hq, k.shape[1], d, cu_seqlens.numel() - 1, int(max_seqlen))
     if softmax_scale is None:
         softmax_scale = default_scale(d)
     if out is None:
@@ -200,7 +217,8 @@ def prefill(q, k, v, cu_seqlens, max_seqlen: int, softmax_scale: Optional[float]
 
 
 def prefill_backward_workspace_bytes(total_tokens: int, num_q_heads: int) -> int:
-    return int(_load().uattn_prefill_backward_workspace_bytes(int(total_tokens), int(num_q_heads)))
+    sizes = int(total_tokens), int(num_q_heads)
+    return int(_load().uattn_prefill_backward_workspace_bytes(*sizes)) if _fits(*sizes) else 0
 
 
 def prefill_backward(q, k, v, out, dout, lse, cu_seqlens, max_seqlen: int, softmax_scale: Optional[float] = None,
@@ -223,6 +241,7 @@ def prefill_backward(q, k, v, out, dout, lse, cu_seqlens, max_seqlen: int, softm
           "lse must be [T,Hq] fp32 on the GPU")
     _need(cu_seqlens.dtype == torch.int32 and cu_seqlens.is_cuda and cu_seqlens.is_contiguous(),
           "cu_seqlens must be contiguous int32 on the GPU")
+    _sizes(T, hq, hkv, d, cu_seqlens.numel() - 1, int(max_seqlen))
     if softmax_scale is None:
         softmax_scale = default_scale(d)
     outs = []
@@ -245,7 +264,8 @@ def prefill_backward(q, k, v, out, dout, lse, cu_seqlens, max_seqlen: int, softm
 
 
 def decode_workspace_bytes(batch: int, max_seqlen: int, num_q_heads: int, head_dim: int) -> int:
-    return int(_load().uattn_decode_workspace_bytes(batch, max_seqlen, num_q_heads, head_dim))
+    sizes = batch, max_seqlen, num_q_heads, head_dim
+    return int(_load().uattn_decode_workspace_bytes(*sizes)) if _fits(*sizes) else 0
 
 
 def new_workspace(nbytes: int, device="cuda"):
@@ -317,6 +337,7 @@ def decode(q, k_pages, v_pages, block_table, seqlens, max_seqlen: int, softmax_s
     _i32_cuda(block_table, "block_table")
     _i32_cuda(seqlens, "seqlens")
     _need(block_table.dim() == 2 and block_table.shape[0] == B and seqlens.shape == (B,), "block_table/seqlens shape")
+    _sizes(B, block_table.shape[1], page, k_pages.shape[0], int(max_seqlen), hq, hkv, d)
     if softmax_scale is None:
         softmax_scale = default_scale(d)
     if out is None:
@@ -361,6 +382,7 @@ def decode_noalloc(q, k_pages, v_pages, block_table, seqlens, max_seqlen: int, s
     _i32_cuda(block_table, "block_table")
     _i32_cuda(seqlens, "seqlens")
     _need(block_table.dim() == 2 and block_table.shape[0] == B and seqlens.shape == (B,), "block_table/seqlens shape")
+    _sizes(B, block_table.shape[1], page, k_pages.shape[0], int(max_seqlen), hq, hkv, d)
     if softmax_scale is None:
         softmax_scale = default_scale(d)
     if out is None:
@@ -386,6 +408,7 @@ def logprob(logits, targets, inv_temperature: float = 1.0, out=None, stream=None
     T, V = logits.shape
     _need(targets.dtype == torch.int32 and targets.is_cuda and targets.shape == (T,) and targets.is_contiguous(),
           "targets must be [T] int32 on the GPU")
+    _sizes(T, V)
     if out is None:
         out = torch.empty(T, dtype=torch.float32, device=logits.device)
     _check(_load().uattn_logprob(_ptr(logits), logits.stride(0), _ptr(targets), T, V, float(inv_temperature),
@@ -416,6 +439,7 @@ def kv_write(k_new, v_new, block_table, seq_idx, positions, k_pages, v_pages, st
     _i32_cuda(positions, "positions", "must be int32 on the GPU")
     _need(block_table.dim() == 2 and seq_idx.shape == (N,) and positions.shape == (N,), "index shapes")
     B, maxp = block_table.shape
+    _sizes(N, B, maxp, page, P, hkv, d)
     _check(_load().uattn_kv_write(_ptr(k_new), _ptr(v_new), k_new.stride(0), _ptr(block_table), _ptr(seq_idx),
                                   _ptr(positions), N, B, maxp, page, P, hkv, d, _ptr(k_pages), _ptr(v_pages),
                                   _stream(stream)))
@@ -425,6 +449,7 @@ def kv_write(k_new, v_new, block_table, seq_idx, positions, k_pages, v_pages, st
 def rope_cache(max_position: int, head_dim: int, theta: float, out=None, stream=None):
     """The NeoX rotary table [max_position, head_dim/2, 2] fp32 (uattn_rope_cache)."""
     import torch
+    _sizes(max_position, head_dim)
     if out is None:
         out = torch.empty((max_position, head_dim // 2, 2), dtype=torch.float32, device="cuda")
     _need(out.dtype == torch.float32 and out.is_cuda and out.is_contiguous()
@@ -453,6 +478,7 @@ def qk_norm_rope(q, k, positions, q_weight, k_weight, cos_sin, eps: float = 1e-6
           "positions must be [T] int32 on the GPU")
     _need(cos_sin.dtype == torch.float32 and cos_sin.is_cuda and cos_sin.is_contiguous() and cos_sin.dim() == 3
           and cos_sin.shape[1:] == (d // 2, 2), "cos_sin must be [max_position, d/2, 2] fp32")
+    _sizes(cos_sin.shape[0], T, hq, hkv, d)
     if q_out is None:
         q_out = torch.empty_like(q)
     if k_out is None:
@@ -475,6 +501,7 @@ def lm_head(hidden, weight, out=None, stream=None):
     T, H = hidden.shape
     V, H2 = weight.shape
     _need(H2 == H, "hidden and weight widths differ")
+    _sizes(T, V, H)
     if out is None:
         stride = (V + 7) // 8 * 8
         out = torch.empty((T, stride), dtype=torch.bfloat16, device=hidden.device)[:, :V]
@@ -485,7 +512,8 @@ def lm_head(hidden, weight, out=None, stream=None):
 
 
 def lm_head_logprob_workspace_bytes(num_rows: int, vocab: int) -> int:
-    return int(_load().uattn_lm_head_logprob_workspace_bytes(int(num_rows), int(vocab)))
+    sizes = int(num_rows), int(vocab)
+    return int(_load().uattn_lm_head_logprob_workspace_bytes(*sizes)) if _fits(*sizes) else 0
 
 
 def lm_head_logprob(hidden, weight, targets, inv_temperature: float = 1.0, out=None, logits=None, workspace=None,
@@ -502,6 +530,7 @@ def lm_head_logprob(hidden, weight, targets, inv_temperature: float = 1.0, out=N
     T, H = hidden.shape
     V, H2 = weight.shape
     _need(H2 == H, "hidden and weight widths differ")
+    _sizes(T, V, H)
     _need(targets.dtype == torch.int32 and targets.is_cuda and targets.shape == (T,) and targets.is_contiguous(),
           "targets must be [T] int32 on the GPU")
     if out is None:
@@ -610,6 +639,8 @@ def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None
     bf16, shape = torch.bfloat16, residual.shape
     _need(len(shape) == 2, "residual must be [T, H]")
     T, H = shape
+    if T > _MOST or H > _MOST:
+        _sizes(T, H)
     _whole(residual, bf16, shape, dev, "residual")
     gate_stride = 0
     if x is None:
@@ -641,7 +672,8 @@ def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None
 
 @functools.lru_cache(maxsize=256)
 def residual_norm_backward_workspace_bytes(num_tokens: int, hidden_dim: int) -> int:
-    return int(_load().uattn_residual_norm_backward_workspace_bytes(int(num_tokens), int(hidden_dim)))
+    sizes = int(num_tokens), int(hidden_dim)
+    return int(_load().uattn_residual_norm_backward_workspace_bytes(*sizes)) if _fits(*sizes) else 0
 
 
 def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=None, post_weight=None, gate=None,
@@ -668,6 +700,8 @@ def residual_norm_backward(dy, dresidual_out, residual_out, pre_weight=None, x=N
     bf16, shape = torch.bfloat16, residual_out.shape
     _need(len(shape) == 2, "residual_out must be [T, H]")
     T, H = shape
+    if T > _MOST or H > _MOST:
+        _sizes(T, H)
     _whole(residual_out, bf16, shape, dev, "residual_out")
     if has_block is None:
         has_block = x is not None
@@ -726,6 +760,8 @@ def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
     _need(ids.dim() == 1, "ids must be [T]")
     _whole(ids, torch.int32, ids.shape, dev, "ids")
     T, (V, H) = ids.shape[0], table.shape
+    if T > _MOST or V > _MOST or H > _MOST:
+        _sizes(T, V, H)
     out = _out_rows(out, table, T, H)
     _check(_load().uattn_embedding(ids.data_ptr(), table.data_ptr(), _row_stride(table), scale, T, V, H, out.data_ptr(),
                                    _row_stride(out), _stream_on(dev)))
@@ -734,7 +770,8 @@ def embedding(ids, table, scale: float = 1.0, out=None, stream=None):
 
 @functools.lru_cache(maxsize=256)
 def embedding_backward_workspace_bytes(num_tokens: int, hidden_dim: int) -> int:
-    return int(_load().uattn_embedding_backward_workspace_bytes(int(num_tokens), int(hidden_dim)))
+    sizes = int(num_tokens), int(hidden_dim)
+    return int(_load().uattn_embedding_backward_workspace_bytes(*sizes)) if _fits(*sizes) else 0
 
 
 def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, accumulate: bool = False, dtype=None,
@@ -756,6 +793,8 @@ def embedding_backward(dout, ids, vocab: int, scale: float = 1.0, grad=None, acc
     T, H = dout.shape
     _whole(ids, torch.int32, (T,), dev, "ids")
     vocab = int(vocab)
+    if T > _MOST or vocab > _MOST or H > _MOST:
+        _sizes(T, vocab, H)
     if grad is None:
         _need(not accumulate, "accumulate needs grad")
         dtype = torch.float32 if dtype is None else dtype
@@ -787,7 +826,10 @@ def _penalty_parts(rows, tokens, history, penalties, dev) -> int:
     _whole(tokens, torch.int32, tokens.shape, dev, "tokens")
     _whole(history, torch.int32, (rows, 3), dev, "history")
     _whole(penalties, torch.float32, (rows, 3), dev, "penalties")
-    return tokens.shape[0]
+    n = tokens.shape[0]
+    if n > _MOST:
+        _sizes(n)
+    return n
 
 
 def _mask_parts(rows, vocab, mask, mask_rows, dev) -> Tuple[int, int]:
@@ -798,6 +840,8 @@ def _mask_parts(rows, vocab, mask, mask_rows, dev) -> Tuple[int, int]:
     import torch
     _rows(mask, torch.int32, dev, "mask")
     masks, words = mask.shape
+    if masks > _MOST:
+        _sizes(masks)
     _need(words >= (vocab + 31) // 32, "mask must have a bit for every vocabulary entry")
     if mask_rows is None:
         _need(masks >= rows, "mask needs a row for every row of logits, or mask_rows")
@@ -825,6 +869,8 @@ def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=N
             return logits_process(logits, tokens, history, penalties, bias_ids, bias_values, bias_rows, mask, mask_rows, out)
     _rows(logits, torch.bfloat16, dev, "logits")
     T, V = logits.shape
+    if T > _MOST or V > _MOST:
+        _sizes(T, V)
     num_tokens = _penalty_parts(T, tokens, history, penalties, dev)
     num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows, dev)
     num_bias = 0
@@ -837,6 +883,8 @@ def logits_process(logits, tokens=None, history=None, penalties=None, bias_ids=N
         _whole(bias_values, torch.float32, bias_ids.shape, dev, "bias_values")
         _whole(bias_rows, torch.int32, (T, 2), dev, "bias_rows")
         num_bias = bias_ids.shape[0]
+        if num_bias > _MOST:
+            _sizes(num_bias)
     out = _out_rows(out, logits, T, V)
     _check(_load().uattn_logits_process(
         logits.data_ptr(), _row_stride(logits), T, V, _ptr(tokens), num_tokens, _ptr(history), _ptr(penalties),
@@ -861,6 +909,8 @@ def logits_process_backward(dout, logits, tokens=None, history=None, penalties=N
     _rows(logits, torch.bfloat16, dev, "logits")
     _rows(dout, torch.bfloat16, dev, "dout")
     T, V = logits.shape
+    if T > _MOST or V > _MOST:
+        _sizes(T, V)
     _need(dout.shape == (T, V), "dout must be of the logits' shape")
     num_tokens = _penalty_parts(T, tokens, history, penalties, dev)
     num_masks, mask_stride = _mask_parts(T, V, mask, mask_rows, dev)
@@ -886,6 +936,8 @@ def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=N
             return logprob_backward(logits, targets, dlogp, inv_temperature, out)
     _rows(logits, torch.bfloat16, dev, "logits")
     T, V = logits.shape
+    if T > _MOST or V > _MOST:
+        _sizes(T, V)
     _whole(targets, torch.int32, (T,), dev, "targets")
     _whole(dlogp, torch.float32, (T,), dev, "dlogp")
     out = _out_rows(out, logits, T, V)
@@ -925,6 +977,7 @@ class DecodeSteps:
               "seqlens_steps must be [S,B] int32")
         _need(block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.shape[0] == B,
               "block_table must be [B,maxp] int32")
+        _sizes(B, block_table.shape[1], page, k_pages.shape[0], int(max_seqlen), hq, hkv, d)
         if softmax_scale is None:
             softmax_scale = default_scale(d)
         need = decode_workspace_bytes(B, int(max_seqlen), hq, d)
