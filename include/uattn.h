@@ -27,7 +27,9 @@
  *   - integer data that lives on the device (cu_seqlens, seqlens,
  *     block_table, targets) is trusted: it is not read by the host.  Setting
  *     the environment variable UATTN_VALIDATE=1 makes the host copy it back
- *     (synchronously) and check it before launching, for debugging;
+ *     (on `stream`, waiting for what that holds already) and check it before
+ *     launching, for debugging; a call that is being captured into a graph
+ *     cannot be checked so and is refused (UATTN_EINVAL);
  *   - errors are reported by the return code only; nothing is printed and
  *     nothing aborts.  On any non-OK code no kernel was launched, except
  *     UATTN_ELAUNCH, which reports a failure of the launch itself.

@@ -4,8 +4,6 @@
 #include <stdlib.h>
 #include <string.h>
 
-#include <vector>
-
 #include "../../include/uattn.h"
 #include "uattn_internal.h"
 #include "uattn_numerics.h"
@@ -28,32 +26,32 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 // fp32(scale * log2(e)), the one constant both attention paths fold into exp2.
 float exp2_scale(float softmax_scale) { return static_cast<float>(static_cast<double>(softmax_scale) * kLog2e); }
 
-template <class T>
-bool copy_back(std::vector<T>& host, const T* dev, size_t n) {
-  host.resize(n);
-  if (n == 0) return true;
-  return hipMemcpy(host.data(), dev, n * sizeof(T), hipMemcpyDeviceToHost) == hipSuccess;
-}
-
 bool is_finite(float x) { return x - x == 0.f; }
 
-// A device array copied back for UATTN_VALIDATE; host is nullptr where that fails.
+// A device array copied back for UATTN_VALIDATE, behind what the call's stream holds already; host is nullptr where
+// that fails, as in a stream that is being captured, which runs nothing before its graph does.
 template <class T>
 struct Copied {
   T* host;
-  Copied(const T* dev, size_t n) : host(static_cast<T*>(malloc(n > 0 ? n * sizeof(T) : 1))) {
-    if (host != nullptr && n > 0 && hipMemcpy(host, dev, n * sizeof(T), hipMemcpyDeviceToHost) != hipSuccess) {
-      free(host);
-      host = nullptr;
-    }
+  Copied(const T* dev, size_t n, void* stream) : host(static_cast<T*>(malloc(n > 0 ? n * sizeof(T) : 1))) {
+    if (host == nullptr || n == 0) return;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone &&
+        hipMemcpyAsync(host, dev, n * sizeof(T), hipMemcpyDeviceToHost, st) == hipSuccess &&
+        hipStreamSynchronize(st) == hipSuccess)
+      return;
+    (void)hipGetLastError();  // not the next launch's error
+    free(host);
+    host = nullptr;
   }
   ~Copied() { free(host); }
   Copied(const Copied&) = delete;
   Copied& operator=(const Copied&) = delete;
 };
 
-bool all_below(const int32_t* dev, int32_t n, int32_t limit) {
-  Copied<int32_t> c(dev, static_cast<size_t>(n));
+bool all_below(const int32_t* dev, int32_t n, int32_t limit, void* stream) {
+  Copied<int32_t> c(dev, static_cast<size_t>(n), stream);
   if (c.host == nullptr) return false;
   for (int32_t i = 0; i < n; ++i)
     if (c.host[i] >= limit) return false;
@@ -69,8 +67,8 @@ constexpr int32_t kMaxEmbeddingWidth = 1 << 20;
 constexpr int32_t kMaxListed = 1 << 30;
 
 // Ranges [begin, end) of `width` columns: column 0 to the last ascending, inside [0, limit].
-bool ranges_ok(const int32_t* dev, int32_t rows, int width, int32_t limit) {
-  Copied<int32_t> c(dev, static_cast<size_t>(rows) * width);
+bool ranges_ok(const int32_t* dev, int32_t rows, int width, int32_t limit, void* stream) {
+  Copied<int32_t> c(dev, static_cast<size_t>(rows) * width, stream);
   if (c.host == nullptr) return false;
   for (size_t r = 0; r < static_cast<size_t>(rows); ++r) {
     int32_t least = 0;
@@ -83,8 +81,28 @@ bool ranges_ok(const int32_t* dev, int32_t rows, int width, int32_t limit) {
   return true;
 }
 
+// Targets inside the vocabulary.
+bool targets_ok(const int32_t* dev, int32_t n, int32_t vocab, void* stream) {
+  Copied<int32_t> c(dev, static_cast<size_t>(n), stream);
+  if (c.host == nullptr) return false;
+  for (int32_t i = 0; i < n; ++i)
+    if (c.host[i] < 0 || c.host[i] >= vocab) return false;
+  return true;
+}
+
+// Offsets of packed sequences: from 0 to total_tokens, no sequence longer than max_seqlen.
+bool offsets_ok(const int32_t* dev, int32_t num_seqs, int32_t total_tokens, int32_t max_seqlen, void* stream) {
+  Copied<int32_t> c(dev, static_cast<size_t>(num_seqs) + 1, stream);
+  if (c.host == nullptr || c.host[0] != 0 || c.host[num_seqs] != total_tokens) return false;
+  for (int32_t s = 0; s < num_seqs; ++s) {
+    const int64_t len = static_cast<int64_t>(c.host[s + 1]) - c.host[s];
+    if (len < 0 || len > max_seqlen) return false;
+  }
+  return true;
+}
+
 // What the logit processing and its gradient ask of their common arguments.
-uattn_status check_logits(const uattn::LogitsLaunch& a) {
+uattn_status check_logits(const uattn::LogitsLaunch& a, void* stream) {
   if (a.num_rows < 0 || a.vocab <= 0 || a.num_tokens < 0 || a.num_bias < 0 || a.num_masks < 0) return UATTN_EINVAL;
   if (a.logits_stride < a.vocab || (a.logits_stride % 8) != 0 || a.out_stride < a.vocab || (a.out_stride % 8) != 0)
     return UATTN_EINVAL;
@@ -98,9 +116,9 @@ uattn_status check_logits(const uattn::LogitsLaunch& a) {
   if (a.num_rows == 0) return UATTN_OK;
   if (!a.logits || !a.out || !aligned16(a.logits) || !aligned16(a.out)) return UATTN_EINVAL;
   if (validate_env()) {
-    if (a.history != nullptr && !ranges_ok(a.history, a.num_rows, 3, a.num_tokens)) return UATTN_EINVAL;
-    if (a.bias_rows != nullptr && !ranges_ok(a.bias_rows, a.num_rows, 2, a.num_bias)) return UATTN_EINVAL;
-    if (a.mask != nullptr && a.mask_rows != nullptr && !all_below(a.mask_rows, a.num_rows, a.num_masks))
+    if (a.history != nullptr && !ranges_ok(a.history, a.num_rows, 3, a.num_tokens, stream)) return UATTN_EINVAL;
+    if (a.bias_rows != nullptr && !ranges_ok(a.bias_rows, a.num_rows, 2, a.num_bias, stream)) return UATTN_EINVAL;
+    if (a.mask != nullptr && a.mask_rows != nullptr && !all_below(a.mask_rows, a.num_rows, a.num_masks, stream))
       return UATTN_EINVAL;
   }
   return UATTN_OK;
@@ -148,15 +166,7 @@ uattn_status uattn_prefill(const void* q, const void* k, const void* v, const in
   if (num_seqs == 0 || total_tokens == 0 || max_seqlen == 0) return UATTN_OK;
   if (!q || !k || !v || !cu_seqlens || !out) return UATTN_EINVAL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return UATTN_EINVAL;
-  if (validate_env()) {
-    std::vector<int32_t> cu;
-    if (!copy_back(cu, cu_seqlens, static_cast<size_t>(num_seqs) + 1)) return UATTN_EINVAL;
-    if (cu[0] != 0 || cu[num_seqs] != total_tokens) return UATTN_EINVAL;
-    for (int32_t s = 0; s < num_seqs; ++s) {
-      const int32_t len = cu[s + 1] - cu[s];
-      if (len < 0 || len > max_seqlen) return UATTN_EINVAL;
-    }
-  }
+  if (validate_env() && !offsets_ok(cu_seqlens, num_seqs, total_tokens, max_seqlen, stream)) return UATTN_EINVAL;
   uattn::PrefillLaunch a;
   a.q = q;
   a.k = k;
@@ -190,7 +200,7 @@ uattn_status decode_prepare(const void* q, const void* k_pages, const void* v_pa
                             const int32_t* seqlens, int32_t batch, int32_t max_pages_per_seq, int32_t page_size,
                             int32_t num_pages, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
                             int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
-                            size_t workspace_bytes, DecodeLaunch* launch) {
+                            size_t workspace_bytes, void* stream, DecodeLaunch* launch) {
   if (batch < 0 || max_pages_per_seq < 0 || max_seqlen < 0 || num_pages < 0 || num_q_heads <= 0 ||
       num_kv_heads <= 0)
     return UATTN_EINVAL;
@@ -212,16 +222,16 @@ uattn_status decode_prepare(const void* q, const void* k_pages, const void* v_pa
   if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return UATTN_EWORKSPACE;
   const int64_t nchunk = (static_cast<int64_t>(max_seqlen) + kChunkKeys - 1) / kChunkKeys;
   if (validate_env()) {
-    std::vector<int32_t> sl, bt;
-    if (!copy_back(sl, seqlens, static_cast<size_t>(batch))) return UATTN_EINVAL;
-    if (!copy_back(bt, block_table, static_cast<size_t>(batch) * max_pages_per_seq)) return UATTN_EINVAL;
+    Copied<int32_t> sl(seqlens, static_cast<size_t>(batch), stream);
+    Copied<int32_t> bt(block_table, static_cast<size_t>(batch) * max_pages_per_seq, stream);
+    if (sl.host == nullptr || bt.host == nullptr) return UATTN_EINVAL;
     for (int32_t b = 0; b < batch; ++b) {
-      if (sl[b] < 1 || sl[b] > max_seqlen) return UATTN_EINVAL;
-      const int32_t used = (sl[b] + page_size - 1) / page_size;
-      for (int32_t j = 0; j < used; ++j)
-        if (bt[static_cast<size_t>(b) * max_pages_per_seq + j] < 0 ||
-            bt[static_cast<size_t>(b) * max_pages_per_seq + j] >= num_pages)
-          return UATTN_EINVAL;
+      if (sl.host[b] < 1 || sl.host[b] > max_seqlen) return UATTN_EINVAL;
+      const int32_t used = (sl.host[b] + page_size - 1) / page_size;
+      for (int32_t j = 0; j < used; ++j) {
+        const int32_t pg = bt.host[static_cast<size_t>(b) * max_pages_per_seq + j];
+        if (pg < 0 || pg >= num_pages) return UATTN_EINVAL;
+      }
     }
   }
   DecodeLaunch a;
@@ -275,7 +285,7 @@ uattn_status uattn_decode(const void* q, const void* k_pages, const void* v_page
   const uattn_status st =
       uattn::decode_prepare(q, k_pages, v_pages, block_table, seqlens, batch, max_pages_per_seq, page_size, num_pages,
                             max_seqlen, num_q_heads, num_kv_heads, head_dim, softmax_scale, out, lse, workspace,
-                            workspace_bytes, &a);
+                            workspace_bytes, stream, &a);
   if (st != UATTN_OK || a.batch == 0) return st;
   return uattn::launch_decode(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
@@ -286,12 +296,7 @@ uattn_status uattn_logprob(const void* logits, int64_t row_stride, const int32_t
   if (num_rows == 0) return UATTN_OK;
   if (!logits || !targets || !logp) return UATTN_EINVAL;
   if (!aligned16(logits) || (row_stride % 8) != 0) return UATTN_EINVAL;
-  if (validate_env()) {
-    std::vector<int32_t> tg;
-    if (!copy_back(tg, targets, static_cast<size_t>(num_rows))) return UATTN_EINVAL;
-    for (int32_t t : tg)
-      if (t < 0 || t >= vocab) return UATTN_EINVAL;
-  }
+  if (validate_env() && !targets_ok(targets, num_rows, vocab, stream)) return UATTN_EINVAL;
   uattn::LogprobLaunch a;
   a.logits = logits;
   a.row_stride = row_stride;
@@ -315,15 +320,15 @@ uattn_status uattn_kv_write(const void* k_new, const void* v_new, int64_t token_
   if (!k_new || !v_new || !block_table || !seq_idx || !positions || !k_pages || !v_pages) return UATTN_EINVAL;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages)) return UATTN_EINVAL;
   if (validate_env()) {
-    std::vector<int32_t> si, ps, bt;
-    if (!copy_back(si, seq_idx, static_cast<size_t>(num_tokens)) ||
-        !copy_back(ps, positions, static_cast<size_t>(num_tokens)) ||
-        !copy_back(bt, block_table, static_cast<size_t>(batch) * max_pages_per_seq))
-      return UATTN_EINVAL;
+    Copied<int32_t> si(seq_idx, static_cast<size_t>(num_tokens), stream);
+    Copied<int32_t> ps(positions, static_cast<size_t>(num_tokens), stream);
+    Copied<int32_t> bt(block_table, static_cast<size_t>(batch) * max_pages_per_seq, stream);
+    if (si.host == nullptr || ps.host == nullptr || bt.host == nullptr) return UATTN_EINVAL;
     for (int32_t n = 0; n < num_tokens; ++n) {
-      if (ps[n] < 0) continue;
-      if (si[n] < 0 || si[n] >= batch || ps[n] / page_size >= max_pages_per_seq) return UATTN_EINVAL;
-      const int32_t pg = bt[static_cast<size_t>(si[n]) * max_pages_per_seq + ps[n] / page_size];
+      const int32_t seq = si.host[n], pos = ps.host[n];
+      if (pos < 0) continue;
+      if (seq < 0 || seq >= batch || pos / page_size >= max_pages_per_seq) return UATTN_EINVAL;
+      const int32_t pg = bt.host[static_cast<size_t>(seq) * max_pages_per_seq + pos / page_size];
       if (pg < 0 || pg >= num_pages) return UATTN_EINVAL;
     }
   }
@@ -431,12 +436,7 @@ uattn_status uattn_lm_head_logprob(const void* hidden, int64_t hidden_stride, co
   const size_t need = uattn_lm_head_logprob_workspace_bytes(num_rows, vocab);
   if (workspace == nullptr || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 3u) != 0)
     return UATTN_EWORKSPACE;
-  if (validate_env()) {
-    std::vector<int32_t> tg;
-    if (!copy_back(tg, targets, static_cast<size_t>(num_rows))) return UATTN_EINVAL;
-    for (int32_t t : tg)
-      if (t < 0 || t >= vocab) return UATTN_EINVAL;
-  }
+  if (validate_env() && !targets_ok(targets, num_rows, vocab, stream)) return UATTN_EINVAL;
   uattn::LmHeadLaunch a;
   a.hidden = hidden;
   a.hidden_stride = hidden_stride;
@@ -475,15 +475,7 @@ uattn_status uattn_prefill_backward(const void* q, const void* k, const void* v,
     return UATTN_EINVAL;
   const size_t need = uattn_prefill_backward_workspace_bytes(total_tokens, num_q_heads);
   if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace)) return UATTN_EWORKSPACE;
-  if (validate_env()) {
-    std::vector<int32_t> cu;
-    if (!copy_back(cu, cu_seqlens, static_cast<size_t>(num_seqs) + 1)) return UATTN_EINVAL;
-    if (cu[0] != 0 || cu[num_seqs] != total_tokens) return UATTN_EINVAL;
-    for (int32_t s = 0; s < num_seqs; ++s) {
-      const int32_t len = cu[s + 1] - cu[s];
-      if (len < 0 || len > max_seqlen) return UATTN_EINVAL;
-    }
-  }
+  if (validate_env() && !offsets_ok(cu_seqlens, num_seqs, total_tokens, max_seqlen, stream)) return UATTN_EINVAL;
   uattn::BackwardLaunch a;
   a.q = q;
   a.k = k;
@@ -598,7 +590,7 @@ uattn_status uattn_embedding(const int32_t* ids, const void* table, int64_t tabl
   if (hidden_dim > kMaxEmbeddingWidth) return UATTN_EUNSUPPORTED;
   if (num_tokens == 0) return UATTN_OK;
   if (!ids || !table || !out || !aligned16(table) || !aligned16(out)) return UATTN_EINVAL;
-  if (validate_env() && !all_below(ids, num_tokens, vocab)) return UATTN_EINVAL;
+  if (validate_env() && !all_below(ids, num_tokens, vocab, stream)) return UATTN_EINVAL;
   uattn::EmbeddingLaunch a;
   a.ids = ids;
   a.table = table;
@@ -631,7 +623,7 @@ uattn_status uattn_embedding_backward(const void* dout, int64_t dout_stride, con
   if (num_tokens > 0 && (!dout || !ids || !aligned16(dout))) return UATTN_EINVAL;
   const size_t need = uattn_embedding_backward_workspace_bytes(num_tokens, hidden_dim);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return UATTN_EWORKSPACE;
-  if (validate_env() && !all_below(ids, num_tokens, vocab)) return UATTN_EINVAL;
+  if (validate_env() && !all_below(ids, num_tokens, vocab, stream)) return UATTN_EINVAL;
   uattn::EmbeddingBackwardLaunch a;
   a.dout = dout;
   a.dout_stride = dout_stride;
@@ -673,7 +665,7 @@ uattn_status uattn_logits_process(const void* logits, int64_t logits_stride, int
   a.mask_rows = mask_rows;
   a.out = out;
   a.out_stride = out_stride;
-  const uattn_status st = check_logits(a);
+  const uattn_status st = check_logits(a, stream);
   if (st != UATTN_OK || num_rows == 0) return st;
   return uattn::launch_logits_process(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
@@ -701,7 +693,7 @@ uattn_status uattn_logits_process_backward(const void* dout, int64_t dout_stride
   a.mask_rows = mask_rows;
   a.out = dlogits;
   a.out_stride = dlogits_stride;
-  const uattn_status st = check_logits(a);
+  const uattn_status st = check_logits(a, stream);
   if (st != UATTN_OK || num_rows == 0) return st;
   if (!dout || !aligned16(dout) || dout_stride < vocab || (dout_stride % 8) != 0) return UATTN_EINVAL;
   return uattn::launch_logits_process_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK
@@ -718,8 +710,8 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
   if (num_rows == 0) return UATTN_OK;
   if (!logits || !targets || !dlogp || !dlogits || !aligned16(logits) || !aligned16(dlogits)) return UATTN_EINVAL;
   if (validate_env()) {
-    Copied<int32_t> tg(targets, num_rows);
-    Copied<float> dl(dlogp, num_rows);
+    Copied<int32_t> tg(targets, num_rows, stream);
+    Copied<float> dl(dlogp, num_rows, stream);
     if (tg.host == nullptr || dl.host == nullptr) return UATTN_EINVAL;
     for (int32_t t = 0; t < num_rows; ++t)
       if (dl.host[t] != 0.f && (tg.host[t] < 0 || tg.host[t] >= vocab)) return UATTN_EINVAL;
