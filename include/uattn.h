@@ -580,7 +580,7 @@ uattn_status uattn_logits_process_backward(const void* dout, int64_t dout_stride
  *              dlogp is 0 (a padded or masked token) gets zeros whatever its
  *              logits and target hold
  *   dlogits    [num_rows, dlogits_stride] bf16, first vocab written; 16-byte
- *              aligned, stride a multiple of 8; not logits itself
+ *              aligned, stride a multiple of 8; not logits itself (UATTN_EINVAL)
  *
  * A row whose target is outside [0, vocab), or whose logits are all -inf, gets
  * NaN.  A row is computed by one workgroup in an order that depends only on vocab.

@@ -709,6 +709,7 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
   if (!scale_ok(inv_temperature) || !scale_ok(exp2_scale(inv_temperature))) return UATTN_EINVAL;
   if (num_rows == 0) return UATTN_OK;
   if (!logits || !targets || !dlogp || !dlogits || !aligned16(logits) || !aligned16(dlogits)) return UATTN_EINVAL;
+  if (dlogits == logits) return UATTN_EINVAL;  // every wave reads the target's logit, when others may have written theirs
   if (validate_env()) {
     Copied<int32_t> tg(targets, num_rows, stream);
     Copied<float> dl(dlogp, num_rows, stream);

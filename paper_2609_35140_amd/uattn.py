@@ -926,7 +926,7 @@ def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=N
     """Gradient of logprob with respect to the logits (uattn_logprob_backward).
 
       logits [T, V] bf16 and targets [T] int32 as passed to logprob; dlogp [T] fp32
-      (0: the row gets zeros).  Returns bf16 [T, V].
+      (0: the row gets zeros).  Returns bf16 [T, V]; out may not be logits.
     """
     import torch
     dev = _gpu_of(logits, "logits")

@@ -149,3 +149,11 @@ def test_handle_of_the_default_stream(monkeypatch, handle):
     monkeypatch.setattr(torch.cuda, "stream", lambda stream: stream)
     there = uattn._elsewhere(3, handle)
     assert isinstance(there, Default) and there.device_index == 3
+
+
+def test_logprob_backward_in_place_is_refused(lib):
+    """A workgroup's waves read the target's logit while others write: not in place, whatever the strides."""
+    d = dict(z=P(16), ls=104, tg=P(16), dl=P(16), T=4, V=100, it=1.0, out=P(16), os=104, stream=None)
+    assert _call(lib.uattn_logprob_backward, d, {}) == 1
+    assert _call(lib.uattn_logprob_backward, d, dict(os=112)) == 1
+    assert _call(lib.uattn_logprob_backward, d, dict(T=1)) == 1

@@ -126,3 +126,12 @@ def test_validation_refuses_a_captured_call(ua, monkeypatch):
         graph.replay()
         torch.cuda.synchronize()
         assert bool((marks == n).all()) and torch.equal(rows, table[ids.long()])
+
+
+def test_logprob_backward_in_place_is_refused(ua):
+    import torch
+    z = gu.dev(inputs.normal_bf16((3, 64), 1.0, 363))
+    was = z.clone()
+    with pytest.raises(ua.UattnError, match="EINVAL"):
+        ua.logprob_backward(z, gu.dev_i32([1, 2, 3]), torch.ones(3, device="cuda"), out=z)
+    assert torch.equal(z, was)
