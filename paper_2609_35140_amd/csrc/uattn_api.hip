@@ -102,7 +102,7 @@ bool offsets_ok(const int32_t* dev, int32_t num_seqs, int32_t total_tokens, int3
 }
 
 // What the logit processing and its gradient ask of their common arguments.
-uattn_status check_logits(const uattn::LogitsLaunch& a, void* stream) {
+uattn_status check_logits(const uattn::LogitsLaunch& a, bool grad, void* stream) {
   if (a.num_rows < 0 || a.vocab <= 0 || a.num_tokens < 0 || a.num_bias < 0 || a.num_masks < 0) return UATTN_EINVAL;
   if (a.logits_stride < a.vocab || (a.logits_stride % 8) != 0 || a.out_stride < a.vocab || (a.out_stride % 8) != 0)
     return UATTN_EINVAL;
@@ -115,6 +115,9 @@ uattn_status check_logits(const uattn::LogitsLaunch& a, void* stream) {
   if (a.num_tokens > kMaxListed || a.num_bias > kMaxListed) return UATTN_EUNSUPPORTED;
   if (a.num_rows == 0) return UATTN_OK;
   if (!a.logits || !a.out || !aligned16(a.logits) || !aligned16(a.out)) return UATTN_EINVAL;
+  // in place the rows have to stay where they are: workgroups read others while this one writes
+  const void* in = grad ? a.dout : a.logits;
+  if (in == a.out && (grad ? a.dout_stride : a.logits_stride) != a.out_stride && a.num_rows > 1) return UATTN_EINVAL;
   if (validate_env()) {
     if (a.history != nullptr && !ranges_ok(a.history, a.num_rows, 3, a.num_tokens, stream)) return UATTN_EINVAL;
     if (a.bias_rows != nullptr && !ranges_ok(a.bias_rows, a.num_rows, 2, a.num_bias, stream)) return UATTN_EINVAL;
@@ -665,7 +668,7 @@ uattn_status uattn_logits_process(const void* logits, int64_t logits_stride, int
   a.mask_rows = mask_rows;
   a.out = out;
   a.out_stride = out_stride;
-  const uattn_status st = check_logits(a, stream);
+  const uattn_status st = check_logits(a, false, stream);
   if (st != UATTN_OK || num_rows == 0) return st;
   return uattn::launch_logits_process(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
@@ -693,7 +696,7 @@ uattn_status uattn_logits_process_backward(const void* dout, int64_t dout_stride
   a.mask_rows = mask_rows;
   a.out = dlogits;
   a.out_stride = dlogits_stride;
-  const uattn_status st = check_logits(a, stream);
+  const uattn_status st = check_logits(a, true, stream);
   if (st != UATTN_OK || num_rows == 0) return st;
   if (!dout || !aligned16(dout) || dout_stride < vocab || (dout_stride % 8) != 0) return UATTN_EINVAL;
   return uattn::launch_logits_process_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK

@@ -157,3 +157,13 @@ def test_logprob_backward_in_place_is_refused(lib):
     assert _call(lib.uattn_logprob_backward, d, {}) == 1
     assert _call(lib.uattn_logprob_backward, d, dict(os=112)) == 1
     assert _call(lib.uattn_logprob_backward, d, dict(T=1)) == 1
+
+
+def test_logits_in_place_with_another_stride_is_refused(lib):
+    """Rows would be written over other rows, which other workgroups still read.  One row has no stride."""
+    d = dict(z=P(16), ls=104, T=4, V=100, tok=P(16), N=9, hist=P(16), pen=P(16), bi=P(16), bv=P(16), M=2, br=P(16), mask=P(16),
+             ms=4, K=2, mr=None, out=P(16), os=112, stream=None)
+    assert _call(lib.uattn_logits_process, d, dict(K=4)) == 1
+    d = dict(d=P(16), ds=104, z=P(32), ls=104, T=4, V=100, tok=P(16), N=9, hist=P(16), pen=P(16), mask=P(16), ms=4, K=4,
+             mr=None, out=P(16), os=112, stream=None)
+    assert _call(lib.uattn_logits_process_backward, d, {}) == 1
