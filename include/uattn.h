@@ -385,7 +385,9 @@ uattn_status uattn_prefill_backward(const void* q, const void* k, const void* v,
  *   residual_out = bf16(s),  y = bf16(s * r(s) * pre_weight)
  *
  * in fp32, each output rounded once (the second norm reads s, not its rounding);
- * the mean of a row's squares has to fit fp32.
+ * the mean of a row's squares has to fit fp32.  The norm of the stored
+ * residual_out, by a call without x, is therefore not bit-equal to y: two regimes
+ * that are to agree bit for bit both take y from the call with x.
  *
  *   x             [num_tokens, hidden_dim] bf16, the block's output, or NULL:
  *                 then y is the norm of residual, and post_weight, gate and
@@ -426,7 +428,8 @@ size_t uattn_residual_norm_backward_workspace_bytes(int32_t num_tokens, int32_t 
  *
  *   dy             [num_tokens, hidden_dim] bf16, or NULL where the forward had no y
  *                  (pre_weight, dpre_weight and dy are NULL together)
- *   dresidual_out  [num_tokens, hidden_dim] bf16, or NULL (zeros); not NULL with dy
+ *   dresidual_out  [num_tokens, hidden_dim] bf16, or NULL (zeros); dy and
+ *                  dresidual_out are not both NULL
  *   residual_out   [num_tokens, hidden_dim] bf16, the forward's (the residual
  *                  itself where it had no x); read only with dy
  *   x              as passed to the forward; may be NULL where neither

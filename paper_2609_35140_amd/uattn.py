@@ -629,6 +629,7 @@ def residual_norm(residual, pre_weight=None, x=None, post_weight=None, gate=None
       Every part but residual may be left out, not x and pre_weight both.  Returns
       (residual_out, y): residual itself where there is no x, and None where there
       is no pre_weight.  residual_out may be residual, y may be x (in place).
+      y is the norm of the unrounded s: that of the stored residual_out has other bits.
     """
     import torch
     dev = _gpu_of(residual, "residual")
