@@ -193,16 +193,18 @@ hipError_t launch_logprob_backward(const LogprobBackwardLaunch& a, hipStream_t s
     });
   };
   // Threads and pieces by the vocabulary alone (a row's bits do not depend on the number of rows): four to
-  // nineteen pieces in flight to a thread, and two rows or more to a CU up to 65,536 entries, so that one is
+  // twenty pieces in flight to a thread, and two rows or more to a CU up to 65,536 entries, so that one is
   // read while the other is written.  us for 600 and for 3000 rows: 32,000 entries 512 x 8 17.5 / 71, 256 x 16
   // 18.9 / 73.5; 50,257 512 x 16 28 / 116, 1024 x 8 35 / 136; 8000 128 x 8 8.6 / 17.6, 256 x 4 8.9 / 18.7.
+  // Twenty pieces are what a thread's 128 registers hold (126 used; 21 spill), 163,840 entries of a row: one more
+  // or less in registers costs little (4000 rows: 163,840 entries 508 us with 19, 504 with 20; 140,000 469 and 470).
   using std::integral_constant;
   if (a.vocab <= 2048) return launch(integral_constant<int, 64>{}, integral_constant<int, 4>{});
   if (a.vocab <= 8192) return launch(integral_constant<int, 128>{}, integral_constant<int, 8>{});
   if (a.vocab <= 32768) return launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
   if (a.vocab <= 65536) return launch(integral_constant<int, 512>{}, integral_constant<int, 16>{});
   if (a.vocab <= 131072) return launch(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
-  return launch(integral_constant<int, 1024>{}, integral_constant<int, 19>{});
+  return launch(integral_constant<int, 1024>{}, integral_constant<int, 20>{});
 }
 
 }  // namespace uattn

@@ -510,3 +510,15 @@ def test_binding_refuses(ua):
               lambda: ua.logprob_backward(z, tg, dl, 3e38), lambda: ua.logits_process_backward(odd, odd)):
         with pytest.raises(ua.UattnError):
             f()
+
+
+@pytest.mark.parametrize("V", [155648, 155656, 163832, 163847, 172040])
+def test_logprob_gradient_around_what_registers_hold(ua, V):
+    """Vocabularies whose rows just fit a workgroup's registers, and whose last pieces are read again."""
+    z = inputs.normal_bf16((3, V), 2.5, 359, V)
+    z[0, -9:] = 0xFF80
+    z[1, -1] = 0x4120                       # 10: the maximum in the last piece
+    tg, dl = np.array([V - 10, V - 1, 5]), np.array([1.0, -2.0, 0.5], dtype=np.float32)
+    got = gu.host_f64(ua.logprob_backward(_rows(z)[:, :V], gu.dev_i32(tg), _f32(dl), 0.9))
+    want, err = oracle.logprob_backward_fp64(oracle.bf16_to_f64(z), tg, dl, 0.9)
+    assert np.all(np.abs(got - want) <= (HALF + U) * np.abs(want) + err + 2.0 ** -133)
