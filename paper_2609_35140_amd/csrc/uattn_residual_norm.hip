@@ -120,7 +120,10 @@ __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kern
 // mean(c m) in a second.  The column sums stay in registers over all rows of the workgroup; the
 // workgroup's row groups add theirs through LDS, one set of sums to a workgroup goes to the
 // workspace, and a second kernel adds the sets.  Which rows share a set depends on the numbers of
-// tokens and columns alone.
+// tokens and columns alone.  Its outputs go through the caches whatever their size (us, so / past them:
+// 9815 x 4096 111 / 114, 39,855 x 1024 111 / 112, 39,855 x 4096 389 / 400, 12,000 x 8192 245 / 252, 6000 x 16,384
+// 368 / 365, and the same with a reader of both).  Two pieces to a thread take the 128 registers that sixteen
+// waves leave and spill 24.
 constexpr int kGradWaves = 16, kGradThreads = 64 * kGradWaves;
 constexpr int kMaxSets = 256;
 
@@ -131,7 +134,6 @@ struct NormGradParams {
   int64_t gate_stride;
   float scale, eps, inv_hidden;
   int32_t num_tokens, hidden;
-  bool stream;                // the rows past the caches
   int32_t row_waves, groups;  // waves to a row, rows to a workgroup at a time
   int32_t pre_at, post_at, gate_at;  // which of the sums each is, or -1
 };
@@ -270,7 +272,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
           ds[i][e] = __builtin_fmaf(r, __builtin_fmaf(-n, dot, dy[e] * w[e]), ds[i][e]);
         }
       }
-      if (here && piece(i) < pieces) store16_as(p.stream, p.dresidual, row * pieces, piece(i), pack8(ds[i]));
+      if (here && piece(i) < pieces) store16(p.dresidual, row * pieces, piece(i), pack8(ds[i]));
     }
     if (p.dx == nullptr) continue;
     float cm = 0.f;
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
         }
         if constexpr (kVecs > 1)
           if (p.gate_at >= 0) add_held(1, i, t);
-        if (p.dgate_rows != nullptr && piece(i) < pieces) store16_as(p.stream, p.dgate_rows, row * pieces, piece(i), pack8(t));
+        if (p.dgate_rows != nullptr && piece(i) < pieces) store16(p.dgate_rows, row * pieces, piece(i), pack8(t));
       }
       if (p.post != nullptr) {
         if constexpr (kVecs > 1) {
@@ -331,7 +333,7 @@ __global__ __launch_bounds__(kGradThreads) void residual_norm_grad_kernel(NormGr
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
-      if (here && piece(i) < pieces) store16_as(p.stream, p.dx, row * pieces, piece(i), pack8(ds[i]));
+      if (here && piece(i) < pieces) store16(p.dx, row * pieces, piece(i), pack8(ds[i]));
   }
   // the row groups' column sums, in the groups' order, by the first of them
   auto put = [&](int at, const float(&d)[8], int v) {
@@ -472,7 +474,6 @@ hipError_t launch_residual_norm_backward(const ResidualNormBackwardLaunch& a, hi
   p.inv_hidden = 1.0f / a.hidden_dim;
   p.num_tokens = a.num_tokens;
   p.hidden = a.hidden_dim;
-  p.stream = streams(a.num_tokens, a.hidden_dim);
   FoldParams f{};
   f.parts = p.parts;
   f.sets = norm_sets(a.num_tokens, a.hidden_dim);

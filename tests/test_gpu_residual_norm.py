@@ -256,3 +256,84 @@ def test_binding_refuses(ua):
               lambda: ua.residual_norm_backward(t, t, t, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(ua.UattnError):
             f()
+
+
+BOTH = [(True, True, "shared", True), (True, True, "token", True)]
+
+
+@pytest.mark.parametrize("T,H", [(4500, 64), (2100, 1024), (1100, 4096), (700, 8192), (300, 12008), (515, 16384)])
+@pytest.mark.parametrize("form", BOTH + [(False, False, "none", True)])
+def test_gradient_of_more_rows_than_workgroups_take_at_once(ua, T, H, form):
+    """Column sums carried over rounds of rows, the last one ragged, in workgroups of sixteen rows at a time down to one."""
+    d, r, k = _case(T, H, form, seed=20)
+    got = dict(zip(("dresidual", "dx", "dpre", "dpost", "dgate"), _backward(ua, d, k, d["residual"])))
+    val, mag = oracle.residual_norm_backward_fp64(r["dy"], r["dres"], r["residual"], r["pre"], r["x"], r["post"], r["gate"],
+                                                  block=form[0], **k)
+    assert {n for n, t in got.items() if t is not None} == set(val)
+    for name, want in val.items():
+        # roundings counted as for fewer rows: 512 of a row's norms; a group's rows one after another and at most 256 groups
+        if got[name].dim() == 1:
+            have, bound = got[name].cpu().numpy().astype(np.float64), (512 + T / 256 + 256) * U * mag[name]
+        else:
+            have, bound = gu.host_f64(got[name]), (HALF + 4 * U) * np.abs(want) + 512 * U * mag[name]
+        assert np.all(np.abs(have - want) <= bound), name
+
+
+def _large(T, H, gate, seed):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    return {"residual": mk(T, H), "x": mk(T, H), "pre": mk(H), "post": mk(H), "gate": mk(H) if gate == "shared" else mk(T, H),
+            "dy": mk(T, H), "dres": mk(T, H)}
+
+
+def _some_rows(d, at):
+    return {n: t[at].contiguous() if t.dim() == 2 else t for n, t in d.items()}
+
+
+# 64 MB of rows and more, in every width's kernel
+@pytest.mark.parametrize("T,H,gate", [(65600, 512, "shared"), (33000, 1024, "token"), (16500, 2040, "shared"), (8200, 4096, "token"),
+                                      (4104, 8192, "shared"), (2056, 16384, "token")])
+def test_large_forward(ua, T, H, gate):
+    import torch
+    d, k = _large(T, H, gate, 21), dict(scale=0.5, eps=1e-6)
+    h, y = _forward(ua, d, k)
+    _, alone = ua.residual_norm(d["residual"], d["pre"], eps=1e-6)
+    rms = lambda a: 1 / torch.sqrt((a * a).mean(-1, keepdim=True) + float(np.float32(1e-6)))  # noqa: E731
+    x, res = d["x"].double(), d["residual"].double()
+    b = 0.5 * d["gate"].double() * x * rms(x) * d["post"].double()
+    for got, s, size in ((y, res + b, res.abs() + b.abs()), (alone, res, res.abs())):
+        want = s * rms(s) * d["pre"].double()
+        terms = size * rms(s) * d["pre"].double().abs()
+        assert bool(((got.double() - want).abs() <= (HALF + 4 * U) * want.abs() + 128 * U * terms).all())
+    s, size = res + b, res.abs() + b.abs()
+    assert bool(((h.double() - s).abs() <= (HALF + 4 * U) * s.abs() + 64 * U * size).all())
+    for at in (slice(0, 300), slice(T - 77, T)):
+        hs, ys = _forward(ua, _some_rows(d, at), k)
+        assert torch.equal(hs, h[at]) and torch.equal(ys, y[at])
+
+
+@pytest.mark.parametrize("T,H,gate", [(33000, 1024, "token"), (8200, 4096, "shared"), (2056, 16384, "shared")])
+def test_large_gradient(ua, T, H, gate):
+    import torch
+    d, k = _large(T, H, gate, 22), dict(scale=0.5, eps=1e-6)
+    got = _backward(ua, d, k, d["residual"])
+    for at in (slice(0, 300), slice(T - 77, T)):
+        part = _some_rows(d, at)
+        few = _backward(ua, part, k, part["residual"])
+        for i in (0, 1) + ((4,) if gate == "token" else ()):
+            assert torch.equal(few[i], got[i][at])
+    # the columns' sums, in float64 on the GPU; b of the rows' own float64 gradient
+    rms = lambda a: 1 / torch.sqrt((a * a).mean(-1, keepdim=True) + float(np.float32(1e-6)))  # noqa: E731
+    h, dy, x, post, g = (d[n].double() for n in ("residual", "dy", "x", "post", "gate"))
+    n, a, m = h * rms(h), dy * d["pre"].double(), x * rms(x)
+    mean = (a * n).mean(-1, keepdim=True)
+    ds = d["dres"].double() + rms(h) * (a - n * mean)
+    m_ds = d["dres"].double().abs() + rms(h) * (a.abs() + n.abs() * (a * n).abs().mean(-1, keepdim=True))
+    sums = {2: (dy * n, (dy * n).abs()), 3: (0.5 * ds * g * m, 0.5 * m_ds * (g * m).abs())}
+    if gate == "shared":
+        sums[4] = (0.5 * ds * m * post, 0.5 * m_ds * (m * post).abs())
+    for i, (terms, size) in sums.items():
+        bound = (512 + T / 256 + 256) * U * size.sum(0)
+        assert bool(((got[i].double() - terms.sum(0)).abs() <= bound).all()), i
