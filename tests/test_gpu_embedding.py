@@ -237,3 +237,41 @@ def test_binding_refuses(ua):
               lambda: ua.embedding_backward(t, ids, 4, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(ua.UattnError):
             f()
+
+
+@pytest.mark.parametrize("fp32", [True, False])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_large_gradient(ua, fp32, accumulate):
+    """256 MB of rows: read past the caches, added to a table or written whole; fp64 sums on the GPU."""
+    import torch
+    T, V, H = 65536, 20000, 2048
+    g = torch.Generator(device="cuda")
+    g.manual_seed(323)
+    dout = torch.randn((T, H), generator=g, device="cuda").to(torch.bfloat16)
+    ids = gu.dev_i32(_ids("zipf", T, V))
+    base = torch.randn((V, H), generator=g, device="cuda").to(torch.float32 if fp32 else torch.bfloat16)
+    got = ua.embedding_backward(dout, ids, V, scale=0.5, grad=base.clone(), accumulate=accumulate)
+    ok = (ids >= 0) & (ids < V)
+    at, x = ids[ok].long(), dout[ok].double() * 0.5
+    start = base.double() if accumulate else torch.zeros((V, H), dtype=torch.float64, device="cuda")
+    want = start.clone().index_add_(0, at, x)
+    mag = start.abs().index_add_(0, at, x.abs())
+    count = torch.bincount(at, minlength=V)[:, None]
+    # a piece's 32 tokens, then the pieces one after another, the sum with the table's value; a half step of the result's type
+    bound = (34 + count / 32) * U * mag + (0.0 if fp32 else HALF) * want.abs()
+    assert bool(((got.double() - want).abs() <= bound).all())
+    assert torch.equal(got[count[:, 0] == 0].double(), start[count[:, 0] == 0])
+
+
+def test_large_lookup(ua):
+    """64 MB of rows: written past the caches, into rows of a wider buffer."""
+    import torch
+    T, V, H = 8300, 5000, 4096
+    table = torch.randn((V, H), device="cuda").to(torch.bfloat16)
+    ids = gu.dev_i32(_ids("uniform", T, V))
+    out = torch.full((T, H + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    ua.embedding(ids, table, out=out[:, :H])
+    at = ids.long()
+    known = (at >= 0) & (at < V)
+    assert torch.equal(out[known, :H], table[at[known]]) and not out[at < 0, :H].any() and bool(torch.isnan(out[at >= V, :H]).all())
+    assert bool((out[:, H:] == 7.0).all())

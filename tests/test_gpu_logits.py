@@ -522,3 +522,21 @@ def test_logprob_gradient_around_what_registers_hold(ua, V):
     got = gu.host_f64(ua.logprob_backward(_rows(z)[:, :V], gu.dev_i32(tg), _f32(dl), 0.9))
     want, err = oracle.logprob_backward_fp64(oracle.bf16_to_f64(z), tg, dl, 0.9)
     assert np.all(np.abs(got - want) <= (HALF + U) * np.abs(want) + err + 2.0 ** -133)
+
+
+def test_large_gradients_equal_small_ones(ua):
+    """64 MB of logits and more: gradients read and written past the caches have the bits of few rows' calls."""
+    import torch
+    T, V = 270, 151931
+    c = _case(T, V, seed=8)
+    z, d = _rows(c["z"])[:, :V], _device(c, PENALTY + MASK)
+    z[0, :4] = 1.0
+    tg, dl = gu.dev_i32(inputs.targets(T, V, tag=9)), _f32(inputs.rng(360).standard_normal(T))
+    x = ua.logits_process(z, **_device(c, PENALTY))
+    full = ua.logprob_backward(x, tg, dl, 1.1)
+    back = ua.logits_process_backward(full, z, **d)
+    for at in (slice(0, 90), slice(200, T)):
+        part = dict(d, **{k: d[k][at] for k in ("history", "penalties", "mask_rows")})
+        g = ua.logprob_backward(x[at], tg[at], dl[at], 1.1)
+        assert torch.equal(g.view(torch.int16), full[at].view(torch.int16))
+        assert torch.equal(ua.logits_process_backward(g, z[at], **part).view(torch.int16), back[at].view(torch.int16))
