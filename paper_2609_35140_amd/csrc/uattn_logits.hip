@@ -63,8 +63,8 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
 }
 
-// kOnce: the input passes the caches by, which serve the logits beside it (backward, us: 334 MB of gradient 148 -> 140,
-// 48 MB 32 -> 30; 32 MB that the caches still hold 19.5 -> 21).
+// kOnce: the input passes the caches by, which serve the logits beside it (backward, us, outputs streamed on both sides: 334 MB
+// of gradient 151 -> 148, 304 MB 138 -> 131, 91 MB 54 -> 49, 67 MB 36 -> 37; 32 MB that the caches still hold 18 -> 20).
 template <bool kGrad, bool kBias, bool kOnce>
 __global__ __launch_bounds__(kLogitsThreads, 6) void logits_kernel(LogitsParams p) {
   // counts, and behind them the biases (in their place where the counts serve one row alone)

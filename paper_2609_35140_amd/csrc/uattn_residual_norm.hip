@@ -33,8 +33,8 @@ __device__ __forceinline__ float inverse_rms(float mean, float eps) { return 1.0
 template <int kRowWaves>
 constexpr int kNormWaves = kRowWaves > 4 ? kRowWaves : 4;
 
-// kOnce: the rows pass the caches by, read and written (us: 39,855 x 1024 57 -> 54 with the reads, 8191 x 4096 50 -> 47; but
-// 2000 x 4096, which the caches hold, 12.1 -> 12.6).
+// kOnce: the rows pass the caches by, read and written, from the size on from which outputs do (streams(), with what both
+// sides take: 80 MB 60 -> 54 us, but 33 MB, which the caches hold, 22 -> 24).
 template <int kRowWaves, int kVecs, bool kOnce>
 __global__ __launch_bounds__(64 * kNormWaves<kRowWaves>) void residual_norm_kernel(NormParams p) {
   constexpr int kWaves = kNormWaves<kRowWaves>, kRows = kWaves / kRowWaves;

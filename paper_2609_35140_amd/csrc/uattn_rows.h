@@ -69,11 +69,18 @@ __device__ __forceinline__ void store16_as(bool stream, void* base, int64_t unif
     *to = w;
   }
 }
-// An output of bf16 rows is streamed from 64 MB on: the caches would hand little of it to the operator
-// that reads it next, and lose to it what they hold.  us for an operator and one that reads its output,
-// cached / streamed: residual norm of 4000 x 4096 (33 MB) 39 / 47, of 39,855 x 1024 (82 MB) 112 / 105, of
-// 39,855 x 4096 450 / 439; lookup of 39,855 x 4096 214 / 207 (82 MB: 46 / 48); logits of 3000 x 151,936
-// with the log-prob 529 / 500, of 300 (91 MB) 59 / 61, these with both gradients 169 / 163.
+// An output of bf16 rows is streamed from 64 MB on (residual norm, lookup, logits, the logits' two gradients): the caches
+// would hand little of it to the operator that reads it next, and lose to it what they hold.  One border for all, where
+// they begin to gain; just past it some readers still lose a few percent.  us, cached / streamed, alone and with what
+// reads the output next:
+//   residual norm    4000 x 4096 (33 MB) 22 / 24, 47 / 49; 8600 x 4096 (70 MB) 47 / 48, 96 / 96; 9815 x 4096 (80 MB)
+//                    60 / 54, 120 / 108; 39,855 x 4096 225 / 214, 450 / 428
+//   lookup, norm     8000 x 4096 (66 MB) 18.6 / 16.6, 40 / 40; 39,855 x 1024 (82 MB) 20 / 19, 47 / 47; 24,000 x 4096
+//                    (197 MB) 54 / 49, 127 / 112
+//   logits, log-prob 210 x 151,936 (64 MB) 27 / 26, 41 / 42; 300 (91 MB) 42 / 39, 66 / 69; 1000 (304 MB) 111 / 106,
+//                    176 / 161
+//   log-prob's gradient   222 x 151,936 (67 MB) 28 / 29; 600 (182 MB) 99 / 86; 1302 x 128,256 160 / 148
+//   these four in a row, 151,936 entries: 222 rows 109 / 109, 250 (76 MB) 121 / 126, 300 170 / 168, 1000 466 / 423
 inline bool streams(int64_t rows, int64_t width) { return 2 * rows * width >= int64_t{64} << 20; }
 
 // DPP: every lane reads another of its 16; all lanes of the patterns used have a source.
