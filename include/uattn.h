@@ -592,6 +592,94 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
                                     int32_t num_rows, int32_t vocab, float inv_temperature, void* dlogits,
                                     int64_t dlogits_stride, void* stream);
 
+/*
+ * A KV cache held in 8 or 4 bits.  Keys and values each have k_bits or v_bits, 8 or
+ * 4 (UATTN_EUNSUPPORTED otherwise).  The head_dim elements of a row are cut into
+ * blocks of 32; a block has one scale 2^e, kept as the byte e + 127, and an element
+ * one code:
+ *
+ *   8 bits  sign, 4 exponent bits (bias 7), 3 mantissa bits; at most M = 448
+ *   4 bits  sign, 2 exponent bits (bias 1), 1 mantissa bit; at most M = 6; the even
+ *           element of a pair in the byte's low half
+ *
+ * (E4M3 and E2M1 elements with E8M0 scales.)  e is the smallest whole number with
+ * max|x| <= M * 2^e, -100 at least; the code is the nearest to x * 2^-e, ties to the
+ * even code.  No element is clipped: each is off by at most 2^-4 (8 bits) or 2^-2 (4
+ * bits) of its own size, or half a step at the block's bottom (2^(e-10) or 2^(e-2)).  A block whose largest magnitude is 2^127 or more, or that
+ * holds an infinity or NaN, has the scale byte 255 and reads as NaN throughout.
+ *
+ * The cache is four arrays, codes and scale bytes of keys and of values:
+ *
+ *   k_codes   [num_pages, num_kv_heads, page_size, head_dim * k_bits / 8]  bytes
+ *   k_scales  [num_pages, num_kv_heads, page_size, head_dim / 32]          bytes
+ *   v_codes, v_scales   the same with v_bits
+ *
+ * 16-byte aligned, pages and block_table as uattn_kv_write has them.  The values that
+ * a write's codes stand for are bf16 numbers, and reading them rounds nothing.
+ * head_dim 64 or 128; page_size a power of two >= 16.
+ */
+
+/*
+ * Indexed write of new keys and values into such a cache: uattn_kv_write with the rows
+ * rounded as above.  k_new, v_new, token_stride, block_table, seq_idx, positions and
+ * which tokens are not written: as there.  Every other row keeps its codes and scales.
+ */
+uattn_status uattn_kv_write_mx(const void* k_new, const void* v_new, int64_t token_stride, const int32_t* block_table,
+                               const int32_t* seq_idx, const int32_t* positions, int32_t num_tokens, int32_t batch,
+                               int32_t max_pages_per_seq, int32_t page_size, int32_t num_pages, int32_t num_kv_heads,
+                               int32_t head_dim, int32_t k_bits, int32_t v_bits, void* k_codes, void* k_scales,
+                               void* v_codes, void* v_scales, void* stream);
+
+/*
+ * Rows of such a cache as bf16, packed (what uattn_prefill reads): the keys and values
+ * of the token at positions[n] of sequence seq_idx[n] become row n.
+ *
+ *   seq_idx, positions   [num_tokens] int32.  A token that uattn_kv_write_mx would not
+ *                        write (padding, or without a place in table or pool) gives zeros
+ *   k_out, v_out         token rows of num_kv_heads * head_dim bf16 (written), out_stride
+ *                        elements apart (>= num_kv_heads * head_dim, a multiple of 8);
+ *                        16-byte aligned; what lies between the rows is left alone
+ */
+uattn_status uattn_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales,
+                              int32_t k_bits, int32_t v_bits, const int32_t* block_table, const int32_t* seq_idx,
+                              const int32_t* positions, int32_t num_tokens, int32_t batch, int32_t max_pages_per_seq,
+                              int32_t page_size, int32_t num_pages, int32_t num_kv_heads, int32_t head_dim, void* k_out,
+                              void* v_out, int64_t out_stride, void* stream);
+
+/*
+ * The values that such a cache would hold for packed rows, without a cache: the same
+ * bits as uattn_kv_write_mx and then uattn_kv_read_mx.  The policy update, which
+ * computes keys and values anew, attends to these where the rollout attended to a
+ * cache in 8 or 4 bits (Eq. (1): both regimes the same); uattn_prefill_backward over
+ * them gives the gradient of the rounded rows, which passes to the rows as it is.
+ *
+ *   k, v           token rows of num_kv_heads * head_dim bf16, token_stride elements
+ *                  apart (>= num_kv_heads * head_dim, a multiple of 8); 16-byte aligned
+ *   k_out, v_out   the same with out_stride (written); may be k and v themselves, with
+ *                  the same stride
+ */
+uattn_status uattn_kv_round_mx(const void* k, const void* v, int64_t token_stride, int32_t num_tokens,
+                               int32_t num_kv_heads, int32_t head_dim, int32_t k_bits, int32_t v_bits, void* k_out,
+                               void* v_out, int64_t out_stride, void* stream);
+
+/*
+ * uattn_decode against such a cache: bit for bit what uattn_decode gives for a bf16
+ * cache of the same values, and uattn_prefill for those rows.
+ *
+ *   q, block_table, seqlens, sizes, softmax_scale, out, lse   as uattn_decode's
+ *   workspace   device scratch of at least uattn_decode_workspace_bytes(batch,
+ *               max_seqlen, num_q_heads, head_dim) bytes, 16-byte aligned.  No initial
+ *               contents are needed, and the counters of uattn_decode at its start are
+ *               left alone, so that the two may share one.  Calls that share a workspace
+ *               must be ordered on one stream.
+ */
+uattn_status uattn_decode_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
+                             const void* v_scales, int32_t k_bits, int32_t v_bits, const int32_t* block_table,
+                             const int32_t* seqlens, int32_t batch, int32_t max_pages_per_seq, int32_t page_size,
+                             int32_t num_pages, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
+                             int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

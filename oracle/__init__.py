@@ -29,6 +29,7 @@ from .attention import (  # noqa: F401
     to_bf16_bits,
 )
 from .kv_cache import kv_write  # noqa: F401
+from .kv_mx import code_values, mx_read, mx_round, mx_write  # noqa: F401
 from .lm_head import abs_dot, lm_head_logprob_fp64, logits_bf16, logits_fp64  # noqa: F401
 from .logprob import logprob_fp64  # noqa: F401
 from .norm_rope import qk_norm_rope, rms_norm_bf16, rope_neox, rope_table  # noqa: F401

@@ -37,7 +37,7 @@ TRANS_WAIT = 1
 SGPR_VMEM_WAIT = 5
 
 # the kernel sources that use inline asm
-SOURCES = ("uattn_prefill.hip", "uattn_decode.hip", "uattn_backward.hip", "uattn_lm_head.hip")
+SOURCES = ("uattn_prefill.hip", "uattn_decode.hip", "uattn_decode_mx.hip", "uattn_backward.hip", "uattn_lm_head.hip")
 
 
 def _regs(tok: str) -> set:

@@ -101,6 +101,30 @@ bool offsets_ok(const int32_t* dev, int32_t num_seqs, int32_t total_tokens, int3
   return true;
 }
 
+// Every token that is not padding has a place in the table and the pool.
+bool places_ok(const int32_t* block_table, const int32_t* seq_idx, const int32_t* positions, int32_t num_tokens,
+               int32_t batch, int32_t max_pages_per_seq, int32_t page_size, int32_t num_pages, void* stream) {
+  Copied<int32_t> si(seq_idx, static_cast<size_t>(num_tokens), stream);
+  Copied<int32_t> ps(positions, static_cast<size_t>(num_tokens), stream);
+  Copied<int32_t> bt(block_table, static_cast<size_t>(batch) * max_pages_per_seq, stream);
+  if (si.host == nullptr || ps.host == nullptr || bt.host == nullptr) return false;
+  for (int32_t n = 0; n < num_tokens; ++n) {
+    const int32_t seq = si.host[n], pos = ps.host[n];
+    if (pos < 0) continue;
+    if (seq < 0 || seq >= batch || pos / page_size >= max_pages_per_seq) return false;
+    const int32_t pg = bt.host[static_cast<size_t>(seq) * max_pages_per_seq + pos / page_size];
+    if (pg < 0 || pg >= num_pages) return false;
+  }
+  return true;
+}
+
+bool bits_ok(int32_t k_bits, int32_t v_bits) { return (k_bits == 8 || k_bits == 4) && (v_bits == 8 || v_bits == 4); }
+
+// Token rows of the heads of one tensor, `stride` elements apart.
+bool row_stride_ok(int64_t stride, int32_t num_kv_heads, int32_t head_dim) {
+  return stride >= static_cast<int64_t>(num_kv_heads) * head_dim && stride % 8 == 0;
+}
+
 // What the logit processing and its gradient ask of their common arguments.
 uattn_status check_logits(const uattn::LogitsLaunch& a, bool grad, void* stream) {
   if (a.num_rows < 0 || a.vocab <= 0 || a.num_tokens < 0 || a.num_bias < 0 || a.num_masks < 0) return UATTN_EINVAL;
@@ -322,19 +346,9 @@ uattn_status uattn_kv_write(const void* k_new, const void* v_new, int64_t token_
   if (num_tokens == 0 || batch == 0 || max_pages_per_seq == 0 || num_pages == 0) return UATTN_OK;
   if (!k_new || !v_new || !block_table || !seq_idx || !positions || !k_pages || !v_pages) return UATTN_EINVAL;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages)) return UATTN_EINVAL;
-  if (validate_env()) {
-    Copied<int32_t> si(seq_idx, static_cast<size_t>(num_tokens), stream);
-    Copied<int32_t> ps(positions, static_cast<size_t>(num_tokens), stream);
-    Copied<int32_t> bt(block_table, static_cast<size_t>(batch) * max_pages_per_seq, stream);
-    if (si.host == nullptr || ps.host == nullptr || bt.host == nullptr) return UATTN_EINVAL;
-    for (int32_t n = 0; n < num_tokens; ++n) {
-      const int32_t seq = si.host[n], pos = ps.host[n];
-      if (pos < 0) continue;
-      if (seq < 0 || seq >= batch || pos / page_size >= max_pages_per_seq) return UATTN_EINVAL;
-      const int32_t pg = bt.host[static_cast<size_t>(seq) * max_pages_per_seq + pos / page_size];
-      if (pg < 0 || pg >= num_pages) return UATTN_EINVAL;
-    }
-  }
+  if (validate_env() && !places_ok(block_table, seq_idx, positions, num_tokens, batch, max_pages_per_seq, page_size,
+                                   num_pages, stream))
+    return UATTN_EINVAL;
   uattn::KvWriteLaunch a;
   a.k_new = k_new;
   a.v_new = v_new;
@@ -731,6 +745,135 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
   a.dlogits = dlogits;
   a.dlogits_stride = dlogits_stride;
   return uattn::launch_logprob_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+// ---------------------------------------------------------------------------
+// The cache in 8 or 4 bits
+// ---------------------------------------------------------------------------
+uattn_status uattn_kv_write_mx(const void* k_new, const void* v_new, int64_t token_stride, const int32_t* block_table,
+                               const int32_t* seq_idx, const int32_t* positions, int32_t num_tokens, int32_t batch,
+                               int32_t max_pages_per_seq, int32_t page_size, int32_t num_pages, int32_t num_kv_heads,
+                               int32_t head_dim, int32_t k_bits, int32_t v_bits, void* k_codes, void* k_scales,
+                               void* v_codes, void* v_scales, void* stream) {
+  if (num_tokens < 0 || batch < 0 || max_pages_per_seq < 0 || num_pages < 0 || num_kv_heads <= 0) return UATTN_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return UATTN_EUNSUPPORTED;
+  if (page_size < 16 || (page_size & (page_size - 1)) != 0) return UATTN_EUNSUPPORTED;
+  if (!bits_ok(k_bits, v_bits) || num_kv_heads > 65535) return UATTN_EUNSUPPORTED;
+  if (!row_stride_ok(token_stride, num_kv_heads, head_dim)) return UATTN_EINVAL;
+  if (num_tokens == 0 || batch == 0 || max_pages_per_seq == 0 || num_pages == 0) return UATTN_OK;
+  if (!k_new || !v_new || !block_table || !seq_idx || !positions) return UATTN_EINVAL;
+  if (!k_codes || !k_scales || !v_codes || !v_scales) return UATTN_EINVAL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_codes) || !aligned16(k_scales) || !aligned16(v_codes) ||
+      !aligned16(v_scales))
+    return UATTN_EINVAL;
+  if (validate_env() && !places_ok(block_table, seq_idx, positions, num_tokens, batch, max_pages_per_seq, page_size,
+                                   num_pages, stream))
+    return UATTN_EINVAL;
+  uattn::KvMxLaunch a = {};
+  a.k = k_new;
+  a.v = v_new;
+  a.token_stride = token_stride;
+  a.cache = {k_codes, k_scales, v_codes, v_scales, k_bits, v_bits};
+  a.block_table = block_table;
+  a.seq_idx = seq_idx;
+  a.positions = positions;
+  a.num_tokens = num_tokens;
+  a.batch = batch;
+  a.max_pages_per_seq = max_pages_per_seq;
+  a.page_size = page_size;
+  a.num_pages = num_pages;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  return uattn::launch_kv_write_mx(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales,
+                              int32_t k_bits, int32_t v_bits, const int32_t* block_table, const int32_t* seq_idx,
+                              const int32_t* positions, int32_t num_tokens, int32_t batch, int32_t max_pages_per_seq,
+                              int32_t page_size, int32_t num_pages, int32_t num_kv_heads, int32_t head_dim, void* k_out,
+                              void* v_out, int64_t out_stride, void* stream) {
+  if (num_tokens < 0 || batch < 0 || max_pages_per_seq < 0 || num_pages < 0 || num_kv_heads <= 0) return UATTN_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return UATTN_EUNSUPPORTED;
+  if (page_size < 16 || (page_size & (page_size - 1)) != 0) return UATTN_EUNSUPPORTED;
+  if (!bits_ok(k_bits, v_bits) || num_kv_heads > 65535) return UATTN_EUNSUPPORTED;
+  if (!row_stride_ok(out_stride, num_kv_heads, head_dim)) return UATTN_EINVAL;
+  if (num_tokens == 0) return UATTN_OK;
+  if (!seq_idx || !positions || !k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return UATTN_EINVAL;
+  // without a table or a pool every token is one without a place
+  const bool table = batch > 0 && max_pages_per_seq > 0;
+  if (table && !block_table) return UATTN_EINVAL;
+  if (table && num_pages > 0 && (!k_codes || !k_scales || !v_codes || !v_scales)) return UATTN_EINVAL;
+  if (!aligned16(k_codes) || !aligned16(k_scales) || !aligned16(v_codes) || !aligned16(v_scales)) return UATTN_EINVAL;
+  if (validate_env() && !places_ok(block_table, seq_idx, positions, num_tokens, batch, max_pages_per_seq, page_size,
+                                   num_pages, stream))
+    return UATTN_EINVAL;
+  uattn::KvMxLaunch a = {};
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.out_stride = out_stride;
+  // the kernels of this call only read the cache
+  a.cache = {const_cast<void*>(k_codes), const_cast<void*>(k_scales), const_cast<void*>(v_codes),
+             const_cast<void*>(v_scales), k_bits, v_bits};
+  a.block_table = block_table;
+  a.seq_idx = seq_idx;
+  a.positions = positions;
+  a.num_tokens = num_tokens;
+  a.batch = batch;
+  a.max_pages_per_seq = max_pages_per_seq;
+  a.page_size = page_size;
+  a.num_pages = num_pages;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  return uattn::launch_kv_read_mx(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_kv_round_mx(const void* k, const void* v, int64_t token_stride, int32_t num_tokens,
+                               int32_t num_kv_heads, int32_t head_dim, int32_t k_bits, int32_t v_bits, void* k_out,
+                               void* v_out, int64_t out_stride, void* stream) {
+  if (num_tokens < 0 || num_kv_heads <= 0) return UATTN_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return UATTN_EUNSUPPORTED;
+  if (!bits_ok(k_bits, v_bits) || num_kv_heads > 65535) return UATTN_EUNSUPPORTED;
+  if (!row_stride_ok(token_stride, num_kv_heads, head_dim) || !row_stride_ok(out_stride, num_kv_heads, head_dim))
+    return UATTN_EINVAL;
+  if (num_tokens == 0) return UATTN_OK;
+  if (!k || !v || !k_out || !v_out || !aligned16(k) || !aligned16(v) || !aligned16(k_out) || !aligned16(v_out))
+    return UATTN_EINVAL;
+  // in place the rows have to stay where they are: workgroups read others while this one writes
+  if ((k_out == k || v_out == v) && token_stride != out_stride && num_tokens > 1) return UATTN_EINVAL;
+  if (k_out == v || v_out == k || k_out == v_out) return UATTN_EINVAL;
+  uattn::KvMxLaunch a = {};
+  a.k = k;
+  a.v = v;
+  a.token_stride = token_stride;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.out_stride = out_stride;
+  a.cache.k_bits = k_bits;
+  a.cache.v_bits = v_bits;
+  a.num_tokens = num_tokens;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  return uattn::launch_kv_round_mx(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
+}
+
+uattn_status uattn_decode_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
+                             const void* v_scales, int32_t k_bits, int32_t v_bits, const int32_t* block_table,
+                             const int32_t* seqlens, int32_t batch, int32_t max_pages_per_seq, int32_t page_size,
+                             int32_t num_pages, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
+                             int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  if (!bits_ok(k_bits, v_bits)) return UATTN_EUNSUPPORTED;
+  uattn::DecodeLaunch a;
+  const uattn_status st =
+      uattn::decode_prepare(q, k_codes, v_codes, block_table, seqlens, batch, max_pages_per_seq, page_size, num_pages,
+                            max_seqlen, num_q_heads, num_kv_heads, head_dim, softmax_scale, out, lse, workspace,
+                            workspace_bytes, stream, &a);
+  if (st != UATTN_OK || a.batch == 0) return st;
+  if (!k_scales || !v_scales || !aligned16(k_scales) || !aligned16(v_scales)) return UATTN_EINVAL;
+  // the kernel only reads the cache
+  const uattn::MxCache cache = {const_cast<void*>(k_codes), const_cast<void*>(k_scales), const_cast<void*>(v_codes),
+                                const_cast<void*>(v_scales), k_bits, v_bits};
+  return uattn::launch_decode_mx(a, cache, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
 
 }  // extern "C"

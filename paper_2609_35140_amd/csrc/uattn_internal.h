@@ -73,6 +73,33 @@ struct KvWriteLaunch {
 
 hipError_t launch_kv_write(const KvWriteLaunch& a, hipStream_t stream);
 
+// The pools of a cache held in 8 or 4 bits: codes and scale bytes of keys and values.
+struct MxCache {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+  int32_t k_bits, v_bits;
+};
+
+struct KvMxLaunch {
+  const void* k;         // rows given (write, round)
+  const void* v;
+  int64_t token_stride;
+  void* k_out;           // rows made (read, round)
+  void* v_out;
+  int64_t out_stride;
+  MxCache cache;         // round: the bits alone
+  const int32_t* block_table;
+  const int32_t* seq_idx;
+  const int32_t* positions;
+  int32_t num_tokens, batch, max_pages_per_seq, page_size, num_pages, num_kv_heads, head_dim;
+};
+
+hipError_t launch_kv_write_mx(const KvMxLaunch& a, hipStream_t stream);
+hipError_t launch_kv_read_mx(const KvMxLaunch& a, hipStream_t stream);
+hipError_t launch_kv_round_mx(const KvMxLaunch& a, hipStream_t stream);
+
 struct NormRopeLaunch {
   const void* q;
   const void* k;
@@ -250,6 +277,7 @@ int32_t device_cus();
 // Each returns hipSuccess or the launch error.
 hipError_t launch_prefill(const PrefillLaunch& a, hipStream_t stream);
 hipError_t launch_decode(const DecodeLaunch& a, hipStream_t stream);
+hipError_t launch_decode_mx(const DecodeLaunch& a, const MxCache& cache, hipStream_t stream);  // a's pages and counters unused
 hipError_t launch_logprob(const LogprobLaunch& a, hipStream_t stream);
 
 // Checks uattn_decode's arguments (every rule of uattn.h) and fills the launch

@@ -95,6 +95,14 @@ def _load():
                                                   c_i64, c_i32, c_p, c_p, c_i64, c_p]
     lib.uattn_logprob_backward.restype = c_i32
     lib.uattn_logprob_backward.argtypes = [c_p, c_i64, c_p, c_p, c_i32, c_i32, c_f, c_p, c_i64, c_p]
+    lib.uattn_kv_write_mx.restype = c_i32
+    lib.uattn_kv_write_mx.argtypes = [c_p, c_p, c_i64, c_p, c_p, c_p] + [c_i32] * 9 + [c_p] * 5
+    lib.uattn_kv_read_mx.restype = c_i32
+    lib.uattn_kv_read_mx.argtypes = [c_p] * 4 + [c_i32] * 2 + [c_p] * 3 + [c_i32] * 7 + [c_p, c_p, c_i64, c_p]
+    lib.uattn_kv_round_mx.restype = c_i32
+    lib.uattn_kv_round_mx.argtypes = [c_p, c_p, c_i64] + [c_i32] * 5 + [c_p, c_p, c_i64, c_p]
+    lib.uattn_decode_mx.restype = c_i32
+    lib.uattn_decode_mx.argtypes = [c_p] * 5 + [c_i32] * 2 + [c_p] * 2 + [c_i32] * 8 + [c_f, c_p, c_p, c_p, c_sz, c_p]
     _lib = lib
     return lib
 
@@ -945,6 +953,198 @@ def logprob_backward(logits, targets, dlogp, inv_temperature: float = 1.0, out=N
     _check(_load().uattn_logprob_backward(logits.data_ptr(), _row_stride(logits), targets.data_ptr(), dlogp.data_ptr(), T, V,
                                           inv_temperature, out.data_ptr(), _row_stride(out), _stream_on(dev)))
     return out
+
+
+# ---------------------------------------------------------------------------
+# The KV cache held in 8 or 4 bits.  Its calls run where and as the row-wise
+# operators' do (above).
+# ---------------------------------------------------------------------------
+MX_BLOCK = 32  # elements of a row to a scale
+
+
+def mx_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, k_bits: int = 8, v_bits: int = 8,
+             device="cuda"):
+    """A new cache in k_bits and v_bits (8 or 4): (k_codes, k_scales, v_codes, v_scales), uint8, of zeros.
+
+      codes [num_pages, num_kv_heads, page_size, head_dim * bits / 8], scales [.., head_dim / 32]
+    """
+    import torch
+    _need(k_bits in (8, 4) and v_bits in (8, 4), "k_bits and v_bits are 8 or 4")
+    _need(head_dim in (64, 128), "head_dim is 64 or 128")
+    rows = (num_pages, num_kv_heads, page_size)
+    return tuple(torch.zeros((*rows, width), dtype=torch.uint8, device=device)
+                 for width in (head_dim * k_bits // 8, head_dim // MX_BLOCK, head_dim * v_bits // 8, head_dim // MX_BLOCK))
+
+
+def _mx_pools(k_codes, k_scales, v_codes, v_scales, dev):
+    """(P, Hkv, page, d, k_bits, v_bits) of a cache's four tensors."""
+    import torch
+    u8, shape = torch.uint8, k_scales.shape
+    _need(len(shape) == 4, "scales must be [P,Hkv,page,d/32]")
+    P, hkv, page, blocks = shape
+    d, rows = blocks * MX_BLOCK, shape[:3]
+    wide = k_codes.shape[-1], v_codes.shape[-1]
+    _need(wide[0] in (d, d // 2) and wide[1] in (d, d // 2), "codes must be [P,Hkv,page,d] (8 bits) or [P,Hkv,page,d/2] (4)")
+    _whole(k_scales, u8, shape, dev, "k_scales")
+    _whole(v_scales, u8, shape, dev, "v_scales")
+    _whole(k_codes, u8, (*rows, wide[0]), dev, "k_codes")
+    _whole(v_codes, u8, (*rows, wide[1]), dev, "v_codes")
+    return P, hkv, page, d, 8 if wide[0] == d else 4, 8 if wide[1] == d else 4
+
+
+def _kv_rows(k, v, dev, names):
+    """Elements from token to token of [N,Hkv,d] keys and values whose heads and elements are contiguous."""
+    import torch
+    if k.dim() != 3 or v.shape != k.shape:
+        raise ValueError(f"{names} must be [N,Hkv,d], both the same")
+    n, hkv, d = k.shape
+    for t in (k, v):
+        if t.dtype is not torch.bfloat16 or t.get_device() != dev or (n and (t.stride(2) != 1 or (hkv > 1 and t.stride(1) != d))):
+            raise ValueError(f"{names} must be bfloat16 on GPU {dev} with contiguous heads")
+    if n <= 1:  # torch may report any stride for one token
+        return hkv * d
+    if k.stride(0) != v.stride(0):
+        raise ValueError(f"{names} must have the same token stride")
+    return k.stride(0)
+
+
+def _kv_places(block_table, seq_idx, positions, N, dev):
+    """(B, maxp) of the indices that say where N tokens live."""
+    import torch
+    i32 = torch.int32
+    _need(block_table.dim() == 2, "block_table must be [B,maxp]")
+    _whole(block_table, i32, block_table.shape, dev, "block_table")
+    _whole(seq_idx, i32, (N,), dev, "seq_idx")
+    _whole(positions, i32, (N,), dev, "positions")
+    return block_table.shape
+
+
+def kv_write_mx(k_new, v_new, block_table, seq_idx, positions, k_codes, k_scales, v_codes, v_scales, stream=None):
+    """Write new K/V token rows into a cache in 8 or 4 bits, in place (uattn_kv_write_mx).
+
+      k_new, v_new   [N, Hkv, d] bf16 (token rows may be strided: stride(0) elements apart)
+      block_table    [B, maxp] int32; seq_idx, positions [N] int32 (position < 0: padding)
+      k_codes .. v_scales   the cache (mx_cache), whose widths say in how many bits
+    """
+    dev = _gpu_of(k_codes, "k_codes")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return kv_write_mx(k_new, v_new, block_table, seq_idx, positions, k_codes, k_scales, v_codes, v_scales)
+    P, hkv, page, d, kb, vb = _mx_pools(k_codes, k_scales, v_codes, v_scales, dev)
+    stride = _kv_rows(k_new, v_new, dev, "k_new/v_new")
+    N = k_new.shape[0]
+    _need(k_new.shape[1:] == (hkv, d), "the cache is of other heads")
+    B, maxp = _kv_places(block_table, seq_idx, positions, N, dev)
+    _sizes(N, B, maxp, page, P, hkv, d)
+    _check(_load().uattn_kv_write_mx(k_new.data_ptr(), v_new.data_ptr(), stride, block_table.data_ptr(), seq_idx.data_ptr(),
+                                     positions.data_ptr(), N, B, maxp, page, P, hkv, d, kb, vb, k_codes.data_ptr(),
+                                     k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), _stream_on(dev)))
+    return k_codes, k_scales, v_codes, v_scales
+
+
+def kv_read_mx(k_codes, k_scales, v_codes, v_scales, block_table, seq_idx, positions, k_out=None, v_out=None, stream=None):
+    """Rows of a cache in 8 or 4 bits as bf16 (uattn_kv_read_mx).
+
+      seq_idx, positions [N] int32: row n is the token at positions[n] of sequence seq_idx[n]
+      (zeros for padding, position < 0, and tokens without a place)
+    Returns (k, v) [N, Hkv, d] bf16.
+    """
+    import torch
+    dev = _gpu_of(k_codes, "k_codes")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return kv_read_mx(k_codes, k_scales, v_codes, v_scales, block_table, seq_idx, positions, k_out, v_out)
+    P, hkv, page, d, kb, vb = _mx_pools(k_codes, k_scales, v_codes, v_scales, dev)
+    N = positions.shape[0] if positions.dim() == 1 else -1
+    B, maxp = _kv_places(block_table, seq_idx, positions, N, dev)
+    _sizes(N, B, maxp, page, P, hkv, d)
+    k_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if k_out is None else k_out
+    v_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if v_out is None else v_out
+    stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
+    _need(k_out.shape == (N, hkv, d), "k_out/v_out shape")
+    _check(_load().uattn_kv_read_mx(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), kb, vb,
+                                    block_table.data_ptr(), seq_idx.data_ptr(), positions.data_ptr(), N, B, maxp, page, P, hkv,
+                                    d, k_out.data_ptr(), v_out.data_ptr(), stride, _stream_on(dev)))
+    return k_out, v_out
+
+
+def kv_round_mx(k, v, k_bits: int = 8, v_bits: int = 8, k_out=None, v_out=None, stream=None):
+    """The values that a cache in k_bits and v_bits would hold for packed rows (uattn_kv_round_mx).
+
+      k, v [N, Hkv, d] bf16 (token rows may be strided).  Returns (k_out, v_out), which
+      may be k and v themselves (in place).  The gradient of the rounded rows passes to
+      the rows as it is.
+    """
+    import torch
+    dev = _gpu_of(k, "k")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return kv_round_mx(k, v, k_bits, v_bits, k_out, v_out)
+    _need(k_bits in (8, 4) and v_bits in (8, 4), "k_bits and v_bits are 8 or 4")
+    stride = _kv_rows(k, v, dev, "k/v")
+    N, hkv, d = shape = k.shape
+    _sizes(N, hkv, d)
+    k_out = torch.empty(shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=k.dtype, device=k.device) if v_out is None else v_out
+    out_stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
+    _need(k_out.shape == shape, "k_out/v_out shape")
+    _check(_load().uattn_kv_round_mx(k.data_ptr(), v.data_ptr(), stride, N, hkv, d, k_bits, v_bits, k_out.data_ptr(),
+                                     v_out.data_ptr(), out_stride, _stream_on(dev)))
+    return k_out, v_out
+
+
+def decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max_seqlen: int,
+              softmax_scale: Optional[float] = None, out=None, return_lse: bool = False, lse=None, workspace=None, stream=None):
+    """Token-wise paged decode against a cache in 8 or 4 bits (uattn_decode_mx).
+
+    q [B,Hq,d] bf16; the cache as mx_cache makes it; block_table, seqlens, max_seqlen,
+    out and lse as for :func:`decode`.  ``workspace``: decode_workspace_bytes(...) bytes,
+    whatever they hold (a decode's own may serve); one is allocated when not given.
+    """
+    import torch
+    dev = _gpu_of(q, "q")
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max_seqlen, softmax_scale, out,
+                             return_lse, lse, workspace)
+    _need(q.dim() == 3, "q must be [B,Hq,d]")
+    B, hq, d = q.shape
+    bf16, i32 = torch.bfloat16, torch.int32
+    _whole(q, bf16, q.shape, dev, "q")
+    P, hkv, page, d2, kb, vb = _mx_pools(k_codes, k_scales, v_codes, v_scales, dev)
+    _need(d2 == d, "head_dim mismatch")
+    _need(block_table.dim() == 2 and block_table.shape[0] == B, "block_table must be [B,maxp]")
+    _whole(block_table, i32, block_table.shape, dev, "block_table")
+    _whole(seqlens, i32, (B,), dev, "seqlens")
+    most = int(max_seqlen)
+    _sizes(B, block_table.shape[1], page, P, most, hq, hkv, d)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _whole(out, bf16, q.shape, dev, "out")
+    if lse is not None:
+        _whole(lse, torch.float32, (B, hq), dev, "lse")
+    elif return_lse:
+        lse = q.new_empty((B, hq), dtype=torch.float32)
+    need = _decode_need(B, most, hq, d)
+    if workspace is not None or need:
+        workspace = _workspace(workspace, need, q)
+    _check(_load().uattn_decode_mx(q.data_ptr(), k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
+                                   v_scales.data_ptr(), kb, vb, block_table.data_ptr(), seqlens.data_ptr(), B,
+                                   block_table.shape[1], page, P, most, hq, hkv, d,
+                                   default_scale(d) if softmax_scale is None else softmax_scale, out.data_ptr(), _ptr(lse),
+                                   _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                   _stream_on(dev)))
+    return (out, lse) if lse is not None else out
+
+
+@functools.lru_cache(maxsize=256)
+def _decode_need(batch: int, max_seqlen: int, num_q_heads: int, head_dim: int) -> int:
+    return int(_load().uattn_decode_workspace_bytes(batch, max_seqlen, num_q_heads, head_dim))
 
 
 def raw_call(name: str, *args) -> int:
