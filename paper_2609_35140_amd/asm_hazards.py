@@ -17,6 +17,13 @@ and branch predecessors, looking for the producers of the registers it reads:
 
 Every instruction in between counts one wait state (``s_nop n`` counts n+1).
 
+``scan_matrix`` looks for the compiler's own omissions: a vector or memory
+instruction that reads the result of a 16x16x32 MFMA (4 passes) sooner than 8 wait
+states after it, along any path.  ROCm 7.2.0 leaves the wait states out where an
+``if`` of 8 to 18 wait states stands between the two: it looks back through the
+``if``'s body, marks the block of the MFMA as seen, and does not look along the way
+that skips the body.
+
     python -m paper_2609_35140_amd.asm_hazards            # check the kernels
 """
 from __future__ import annotations
@@ -32,9 +39,11 @@ from . import build as B
 
 TRANS_PREFIXES = ("v_exp_", "v_log_", "v_rcp_", "v_rsq_", "v_sqrt_", "v_sin_", "v_cos_")
 VMEM_PREFIXES = ("global_", "buffer_", "flat_", "scratch_")
+LOAD_PREFIXES = ("ds_read", "global_load", "buffer_load", "flat_load", "scratch_load")
 MFMA_WAIT = 19
 TRANS_WAIT = 1
 SGPR_VMEM_WAIT = 5
+MFMA_16X16X32_WAIT = 8
 
 # the kernel sources that use inline asm
 SOURCES = ("uattn_prefill.hip", "uattn_decode.hip", "uattn_decode_mx.hip", "uattn_backward.hip", "uattn_lm_head.hip")
@@ -148,15 +157,41 @@ def _producers(items, idx, regs, budget, label_sites):
             i -= 1
 
 
+def _label_sites(items):
+    """The branches to each label."""
+    sites = {}
+    for i, it in enumerate(items):
+        if not isinstance(it, tuple) and (it.op.startswith("s_cbranch") or it.op == "s_branch"):
+            sites.setdefault(it.text.split()[-1], []).append(i)
+    return sites
+
+
+def scan_matrix(text: str):
+    """Findings (strings): reads of a 16x16x32 MFMA's result too soon after it."""
+    findings = []
+    for fname, items in _parse(text).items():
+        if not any(not isinstance(it, tuple) and it.op.startswith("v_mfma") for it in items):
+            continue
+        sites = _label_sites(items)
+        for idx, it in enumerate(items):
+            if isinstance(it, tuple) or it.op.startswith(("v_mfma", "s_")):
+                continue
+            read = it.srcs
+            if it.op.startswith(LOAD_PREFIXES):  # (a load's first operand is what it writes)
+                read = set().union(*(_regs(o.split()[0]) for o in it.text.split(None, 1)[1].split(",")[1:] if o.strip()))
+            regs = {r for r in read if r[0] in "va"}
+            for p, d in _producers(items, idx, regs, MFMA_16X16X32_WAIT, sites):
+                if p.op.startswith("v_mfma_f32_16x16x32") and d < MFMA_16X16X32_WAIT:
+                    findings.append(f"{fname}: line {it.line}: '{it.text}' reads the result of '{p.text}' with {d} wait "
+                                    f"states (needs {MFMA_16X16X32_WAIT})")
+    return findings
+
+
 def scan(text: str):
     """Findings (strings) for one assembly text."""
     findings = []
     for fname, items in _parse(text).items():
-        label_sites = {}
-        for i, it in enumerate(items):
-            if not isinstance(it, tuple) and (it.op.startswith("s_cbranch") or it.op == "s_branch"):
-                target = it.text.split()[-1]
-                label_sites.setdefault(target, []).append(i)
+        label_sites = _label_sites(items)
         for idx, it in enumerate(items):
             if isinstance(it, tuple) or not it.asm:
                 continue
@@ -191,12 +226,12 @@ def assembly(src: str) -> str:
             return fh.read()
 
 
-def check(sources=SOURCES):
+def check(sources=SOURCES, scans=(scan, scan_matrix)):
     """{source: findings} for the kernel sources."""
     paths = [os.path.join(B.CSRC, s) for s in sources]
     with ThreadPoolExecutor(max(1, min(len(paths), os.cpu_count() or 1))) as ex:
         texts = list(ex.map(assembly, paths))
-    return {s: scan(t) for s, t in zip(sources, texts)}
+    return {s: [f for one in scans for f in one(t)] for s, t in zip(sources, texts)}
 
 
 def main() -> int:
