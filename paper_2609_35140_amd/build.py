@@ -56,10 +56,12 @@ def sources():
 # Extra flags for single sources.  The backward's dK/dV kernel carries 128 fp32
 # accumulators through its loop; by default the compiler parks them in AGPRs
 # and copies them to VGPRs and back on every iteration (about 200 moves per
-# 128 MFMAs).  Asking for the VGPR form of the MFMAs removes the copies.  Only
-# this file: the flag changes the decode kernel's code too.
+# 128 MFMAs).  Asking for the VGPR form of the MFMAs removes the copies.  Likewise
+# the decode over a cache in 8 or 4 bits (550 moves of 2200 vector instructions a
+# chunk).  Only these files: the flag changes the decode kernel's code too.
 PER_FILE_FLAGS = {
     "uattn_backward.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "uattn_decode_mx.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 OBJDIR = os.path.join(PKG, "_build")

@@ -237,6 +237,50 @@ def test_decode_rising_scores_and_other_scales(ua):
             assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
 
 
+def _many(ua, lens, hq, hkv, d, bits, tag, most=None, sigma=4.0):
+    """Both decodes of sequences given by their lengths (0: none) where all share one long sequence's pages."""
+    long = max(lens)
+    c = Cache([long], hkv, d, 16, bits, tag, sigma=sigma)
+    table = gu.dev_i32(np.repeat(c.table, len(lens), axis=0))
+    q = gu.dev(inputs.normal_bf16((len(lens), hq, d), sigma, 628, tag))
+    got, want = both(ua, c, q, gu.dev_i32(lens), most or long, table=table, scale=0.05)
+    there = np.array(lens) > 0
+    assert np.array_equal(got[0][there], want[0][there]) and np.array_equal(got[1][there], want[1][there])
+    assert np.all(np.isnan(oracle.bf16_to_f64(got[0][~there])))
+    assert not np.any(np.isnan(oracle.bf16_to_f64(got[0][there])))
+
+
+@pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("hq,hkv,d", [(16, 8, 128), (16, 16, 64), (136, 8, 64), (136, 8, 128)])
+def test_decode_many_long_sequences(ua, bits, hq, hkv, d):
+    """More pairs of sequence and kv head than workgroups fit the chip, past eight chunks: lengths around the borders of tiles,
+    chunks and of four chunks, references that move, entries without keys."""
+    n = 1100 // hkv
+    lens = [2100, 1, 0, 64, 65, 1023, 1024, 1025, 257, 2049, 2048, -3, 2304] + list(inputs.rng(640, d).integers(1, 600, n - 13))
+    _many(ua, lens, hq, hkv, d, bits, 60 + hkv)
+
+
+@pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("hq,hkv,d,long", [(4, 2, 128, 2048), (34, 2, 64, 1500), (34, 2, 128, 1500), (16, 1, 64, 300), (8, 1, 128, 900)])
+def test_decode_few_chunks(ua, bits, hq, hkv, d, long):
+    """Up to eight chunks, entries of fewer among them."""
+    _many(ua, [long, 1, 0, 256, 257, long - 1, 64, min(long, 512), 280], hq, hkv, d, bits, 70 + hkv)
+
+
+@pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (17, 1, 128), (5, 1, 64), (32, 1, 64)])
+def test_decode_bound_far_above_the_lengths(ua, bits, hq, hkv, d):
+    """max_seqlen of a million (codes are then read past the caches), lengths of up to eleven chunks."""
+    lens = [2700, 1, 256, 257, 513, 0, 1100]
+    c = Cache([max(lens)], hkv, d, 16, bits, 80, sigma=4.0)
+    table = np.full((len(lens), 1 << 16), -1, dtype=np.int32)
+    table[:, : c.table.shape[1]] = c.table
+    q = gu.dev(inputs.normal_bf16((len(lens), hq, d), 4.0, 629, hq))
+    got, want = both(ua, c, q, gu.dev_i32(lens), 1 << 20, table=gu.dev_i32(table), scale=0.05)
+    there = np.array(lens) > 0
+    assert np.array_equal(got[0][there], want[0][there]) and np.array_equal(got[1][there], want[1][there])
+
+
 def test_decode_nan_blocks_reach_their_rows_alone(ua):
     """Blocks that read as NaN inside a context: NaN for the kv head they are in, as in the bf16 decode; others untouched."""
     lens = [300, 40]
