@@ -663,15 +663,25 @@ uattn_status uattn_kv_round_mx(const void* k, const void* v, int64_t token_strid
                                void* v_out, int64_t out_stride, void* stream);
 
 /*
+ * Bytes of device workspace uattn_decode_mx needs for these sizes: the fp32 partials of
+ * the positional split, at most uattn_decode_workspace_bytes; 0 where no split goes
+ * through memory (up to 2048 keys, with num_q_heads / num_kv_heads <= 16 or head_dim
+ * 64; up to 256 keys otherwise).  Pure host arithmetic; 0 for invalid sizes.
+ */
+size_t uattn_decode_mx_workspace_bytes(int32_t batch, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
+                                       int32_t head_dim);
+
+/*
  * uattn_decode against such a cache: bit for bit what uattn_decode gives for a bf16
  * cache of the same values, and uattn_prefill for those rows.
  *
  *   q, block_table, seqlens, sizes, softmax_scale, out, lse   as uattn_decode's
- *   workspace   device scratch of at least uattn_decode_workspace_bytes(batch,
- *               max_seqlen, num_q_heads, head_dim) bytes, 16-byte aligned.  No initial
- *               contents are needed, and the counters of uattn_decode at its start are
- *               left alone, so that the two may share one.  Calls that share a workspace
- *               must be ordered on one stream.
+ *   workspace   device scratch of at least uattn_decode_mx_workspace_bytes(batch,
+ *               max_seqlen, num_q_heads, num_kv_heads, head_dim) bytes, 16-byte aligned
+ *               (may be NULL when that is 0).  No initial contents are needed.  The
+ *               partials go at its end: one that is large enough for uattn_decode with
+ *               these sizes keeps that call's counters as they are, so that the two may
+ *               share it.  Calls that share a workspace must be ordered on one stream.
  */
 uattn_status uattn_decode_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
                              const void* v_scales, int32_t k_bits, int32_t v_bits, const int32_t* block_table,

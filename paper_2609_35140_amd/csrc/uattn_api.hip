@@ -227,7 +227,7 @@ uattn_status decode_prepare(const void* q, const void* k_pages, const void* v_pa
                             const int32_t* seqlens, int32_t batch, int32_t max_pages_per_seq, int32_t page_size,
                             int32_t num_pages, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
                             int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
-                            size_t workspace_bytes, void* stream, DecodeLaunch* launch) {
+                            size_t workspace_bytes, size_t need, void* stream, DecodeLaunch* launch) {
   if (batch < 0 || max_pages_per_seq < 0 || max_seqlen < 0 || num_pages < 0 || num_q_heads <= 0 ||
       num_kv_heads <= 0)
     return UATTN_EINVAL;
@@ -245,7 +245,6 @@ uattn_status decode_prepare(const void* q, const void* k_pages, const void* v_pa
   if (static_cast<int64_t>(max_pages_per_seq) * page_size < max_seqlen) return UATTN_EINVAL;
   if (!q || !k_pages || !v_pages || !block_table || !seqlens || !out) return UATTN_EINVAL;
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return UATTN_EINVAL;
-  const size_t need = uattn_decode_workspace_bytes(batch, max_seqlen, num_q_heads, head_dim);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return UATTN_EWORKSPACE;
   const int64_t nchunk = (static_cast<int64_t>(max_seqlen) + kChunkKeys - 1) / kChunkKeys;
   if (validate_env()) {
@@ -312,7 +311,7 @@ uattn_status uattn_decode(const void* q, const void* k_pages, const void* v_page
   const uattn_status st =
       uattn::decode_prepare(q, k_pages, v_pages, block_table, seqlens, batch, max_pages_per_seq, page_size, num_pages,
                             max_seqlen, num_q_heads, num_kv_heads, head_dim, softmax_scale, out, lse, workspace,
-                            workspace_bytes, stream, &a);
+                            workspace_bytes, uattn_decode_workspace_bytes(batch, max_seqlen, num_q_heads, head_dim), stream, &a);
   if (st != UATTN_OK || a.batch == 0) return st;
   return uattn::launch_decode(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
@@ -856,6 +855,16 @@ uattn_status uattn_kv_round_mx(const void* k, const void* v, int64_t token_strid
   return uattn::launch_kv_round_mx(a, static_cast<hipStream_t>(stream)) == hipSuccess ? UATTN_OK : UATTN_ELAUNCH;
 }
 
+size_t uattn_decode_mx_workspace_bytes(int32_t batch, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
+                                       int32_t head_dim) {
+  if (batch <= 0 || max_seqlen <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || head_dim <= 0) return 0;
+  if (num_q_heads % num_kv_heads != 0) return 0;
+  const int64_t nchunk = (static_cast<int64_t>(max_seqlen) + kChunkKeys - 1) / kChunkKeys;
+  if (nchunk <= 1 || uattn::decode_mx_in_lds(nchunk, num_q_heads / num_kv_heads, head_dim)) return 0;
+  return uattn::decode_ws_acc_bytes(batch, nchunk, num_q_heads, head_dim) +
+         uattn::decode_ws_ml_bytes(batch, nchunk, num_q_heads);
+}
+
 uattn_status uattn_decode_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
                              const void* v_scales, int32_t k_bits, int32_t v_bits, const int32_t* block_table,
                              const int32_t* seqlens, int32_t batch, int32_t max_pages_per_seq, int32_t page_size,
@@ -863,11 +872,12 @@ uattn_status uattn_decode_mx(const void* q, const void* k_codes, const void* k_s
                              int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
                              size_t workspace_bytes, void* stream) {
   if (!bits_ok(k_bits, v_bits)) return UATTN_EUNSUPPORTED;
+  const size_t need = uattn_decode_mx_workspace_bytes(batch, max_seqlen, num_q_heads, num_kv_heads, head_dim);
   uattn::DecodeLaunch a;
   const uattn_status st =
       uattn::decode_prepare(q, k_codes, v_codes, block_table, seqlens, batch, max_pages_per_seq, page_size, num_pages,
                             max_seqlen, num_q_heads, num_kv_heads, head_dim, softmax_scale, out, lse, workspace,
-                            workspace_bytes, stream, &a);
+                            workspace_bytes, need, stream, &a);
   if (st != UATTN_OK || a.batch == 0) return st;
   if (!k_scales || !v_scales || !aligned16(k_scales) || !aligned16(v_scales)) return UATTN_EINVAL;
   // the kernel only reads the cache

@@ -589,7 +589,7 @@ hipError_t launch(DecodeMxParams p, int num_cus, hipStream_t stream) {
     // Up to kTeamWaves chunks: one launch, nothing through memory.  A step of 700 keys,
     // 32/8 heads, 8 bits 10.7 us with a merge, 9.1 so; 64 entries of 300-2000 keys, 32/8
     // heads 58 and 44.
-    if (p.nchunk_max > 1 && p.nchunk_max <= kTeamWaves)
+    if (p.nchunk_max > 1 && decode_mx_in_lds(p.nchunk_max, p.group, D))
       return run(decode_mx_kernel<D, NB, KB, VB, Split::kFused, 0>, pairs, p.nchunk_max);
     // Many pairs: a workgroup to a pair.  256 entries of 4000 keys, 32/8 heads, 8 bits 436
     // us with partials and their merge, 334 so; of 500-8000 keys in 4 bits 255, 244.  With
@@ -612,6 +612,10 @@ hipError_t launch(DecodeMxParams p, int num_cus, hipStream_t stream) {
 }
 
 }  // namespace
+
+bool decode_mx_in_lds(int64_t nchunk, int64_t group, int64_t head_dim) {
+  return nchunk <= kTeamWaves && (group <= kQCols || head_dim == 64);
+}
 
 hipError_t launch_decode_mx(const DecodeLaunch& a, const MxCache& cache, hipStream_t stream) {
   DecodeMxParams p;

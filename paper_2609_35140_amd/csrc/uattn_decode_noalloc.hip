@@ -70,7 +70,7 @@ uattn_status uattn_decode_noalloc(const void* q, const void* k_pages, const void
   const uattn_status st =
       uattn::decode_prepare(q, k_pages, v_pages, block_table, seqlens, batch, max_pages_per_seq, page_size, num_pages,
                             max_seqlen, num_q_heads, num_kv_heads, head_dim, softmax_scale, out, lse, ws,
-                            ws != nullptr ? kScratchBytes : 0, stream, &a);
+                            ws != nullptr ? kScratchBytes : 0, need, stream, &a);
   if (st != UATTN_OK || a.batch == 0) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.ws_cnt != nullptr) {

@@ -278,17 +278,19 @@ int32_t device_cus();
 hipError_t launch_prefill(const PrefillLaunch& a, hipStream_t stream);
 hipError_t launch_decode(const DecodeLaunch& a, hipStream_t stream);
 hipError_t launch_decode_mx(const DecodeLaunch& a, const MxCache& cache, hipStream_t stream);  // a's pages and counters unused
+// Whether all chunks of an entry are folded in LDS, so that no partial goes through the workspace.
+bool decode_mx_in_lds(int64_t nchunk, int64_t group, int64_t head_dim);
 hipError_t launch_logprob(const LogprobLaunch& a, hipStream_t stream);
 
 // Checks uattn_decode's arguments (every rule of uattn.h) and fills the launch
 // record, laying the workspace out as counters at its start and partials at
-// its end; `stream` orders UATTN_VALIDATE's copies.  Returns the status uattn_decode reports; `launch->batch` is 0
+// its end (`need`: the bytes it has to have); `stream` orders UATTN_VALIDATE's copies.  Returns the status uattn_decode reports; `launch->batch` is 0
 // when there is nothing to launch.
 uattn_status decode_prepare(const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
                             const int32_t* seqlens, int32_t batch, int32_t max_pages_per_seq, int32_t page_size,
                             int32_t num_pages, int32_t max_seqlen, int32_t num_q_heads, int32_t num_kv_heads,
                             int32_t head_dim, float softmax_scale, void* out, float* lse, void* workspace,
-                            size_t workspace_bytes, void* stream, DecodeLaunch* launch);
+                            size_t workspace_bytes, size_t need, void* stream, DecodeLaunch* launch);
 
 // Decode workspace: arrival counters at the start (kept zero between calls),
 // the fp32 partials (acc, then m/l) at the end of the caller's buffer.

@@ -101,6 +101,8 @@ def _load():
     lib.uattn_kv_read_mx.argtypes = [c_p] * 4 + [c_i32] * 2 + [c_p] * 3 + [c_i32] * 7 + [c_p, c_p, c_i64, c_p]
     lib.uattn_kv_round_mx.restype = c_i32
     lib.uattn_kv_round_mx.argtypes = [c_p, c_p, c_i64] + [c_i32] * 5 + [c_p, c_p, c_i64, c_p]
+    lib.uattn_decode_mx_workspace_bytes.restype = c_sz
+    lib.uattn_decode_mx_workspace_bytes.argtypes = [c_i32] * 5
     lib.uattn_decode_mx.restype = c_i32
     lib.uattn_decode_mx.argtypes = [c_p] * 5 + [c_i32] * 2 + [c_p] * 2 + [c_i32] * 8 + [c_f, c_p, c_p, c_p, c_sz, c_p]
     _lib = lib
@@ -976,47 +978,60 @@ def mx_cache(num_pages: int, num_kv_heads: int, page_size: int, head_dim: int, k
                  for width in (head_dim * k_bits // 8, head_dim // MX_BLOCK, head_dim * v_bits // 8, head_dim // MX_BLOCK))
 
 
+# A step's calls are short, so what is right is found right by one expression over all
+# tensors, and which of them is not is looked up only then.
 def _mx_pools(k_codes, k_scales, v_codes, v_scales, dev):
     """(P, Hkv, page, d, k_bits, v_bits) of a cache's four tensors."""
     import torch
-    u8, shape = torch.uint8, k_scales.shape
-    _need(len(shape) == 4, "scales must be [P,Hkv,page,d/32]")
+    u8, shape, ks, vs = torch.uint8, k_scales.shape, k_codes.shape, v_codes.shape
+    if len(shape) != 4 or len(ks) != 4 or len(vs) != 4:
+        raise ValueError("codes must be [P,Hkv,page,d] (8 bits) or [P,Hkv,page,d/2] (4), scales [P,Hkv,page,d/32]")
     P, hkv, page, blocks = shape
-    d, rows = blocks * MX_BLOCK, shape[:3]
-    wide = k_codes.shape[-1], v_codes.shape[-1]
-    _need(wide[0] in (d, d // 2) and wide[1] in (d, d // 2), "codes must be [P,Hkv,page,d] (8 bits) or [P,Hkv,page,d/2] (4)")
-    _whole(k_scales, u8, shape, dev, "k_scales")
-    _whole(v_scales, u8, shape, dev, "v_scales")
-    _whole(k_codes, u8, (*rows, wide[0]), dev, "k_codes")
-    _whole(v_codes, u8, (*rows, wide[1]), dev, "v_codes")
-    return P, hkv, page, d, 8 if wide[0] == d else 4, 8 if wide[1] == d else 4
+    d = blocks * MX_BLOCK
+    kb, vb = 8 if ks[3] == d else 4, 8 if vs[3] == d else 4
+    if not (k_codes.dtype is k_scales.dtype is v_codes.dtype is v_scales.dtype is u8 and v_scales.shape == shape
+            and ks == (P, hkv, page, d * kb // 8) and vs == (P, hkv, page, d * vb // 8)
+            and k_codes.get_device() == k_scales.get_device() == v_codes.get_device() == v_scales.get_device() == dev
+            and k_codes.is_contiguous() and k_scales.is_contiguous() and v_codes.is_contiguous() and v_scales.is_contiguous()):
+        for name, t, width in (("k_scales", k_scales, blocks), ("v_scales", v_scales, blocks), ("k_codes", k_codes, d * kb // 8),
+                               ("v_codes", v_codes, d * vb // 8)):
+            _whole(t, u8, (P, hkv, page, width), dev, name)
+    return P, hkv, page, d, kb, vb
 
 
 def _kv_rows(k, v, dev, names):
     """Elements from token to token of [N,Hkv,d] keys and values whose heads and elements are contiguous."""
     import torch
-    if k.dim() != 3 or v.shape != k.shape:
+    shape, stride, bf16 = k.shape, k.stride(), torch.bfloat16
+    if len(shape) != 3 or v.shape != shape:
         raise ValueError(f"{names} must be [N,Hkv,d], both the same")
-    n, hkv, d = k.shape
+    n, hkv, d = shape
+    if not (k.dtype is bf16 and v.dtype is bf16 and k.get_device() == dev and v.get_device() == dev):
+        raise ValueError(f"{names} must be bfloat16 on GPU {dev}")
+    if v.stride() == stride and stride[1] == d and stride[2] == 1:
+        return stride[0] if n > 1 else hkv * d  # torch may report any stride for one token
     for t in (k, v):
-        if t.dtype is not torch.bfloat16 or t.get_device() != dev or (n and (t.stride(2) != 1 or (hkv > 1 and t.stride(1) != d))):
-            raise ValueError(f"{names} must be bfloat16 on GPU {dev} with contiguous heads")
-    if n <= 1:  # torch may report any stride for one token
+        if n and (t.stride(2) != 1 or (hkv > 1 and t.stride(1) != d)):
+            raise ValueError(f"{names}: heads and their elements must be contiguous")
+    if n <= 1:
         return hkv * d
     if k.stride(0) != v.stride(0):
         raise ValueError(f"{names} must have the same token stride")
-    return k.stride(0)
+    return stride[0]
 
 
 def _kv_places(block_table, seq_idx, positions, N, dev):
     """(B, maxp) of the indices that say where N tokens live."""
     import torch
-    i32 = torch.int32
-    _need(block_table.dim() == 2, "block_table must be [B,maxp]")
-    _whole(block_table, i32, block_table.shape, dev, "block_table")
-    _whole(seq_idx, i32, (N,), dev, "seq_idx")
-    _whole(positions, i32, (N,), dev, "positions")
-    return block_table.shape
+    i32, shape = torch.int32, block_table.shape
+    if len(shape) != 2:
+        raise ValueError("block_table must be [B,maxp]")
+    if not (block_table.dtype is seq_idx.dtype is positions.dtype is i32 and seq_idx.shape == positions.shape == (N,)
+            and block_table.get_device() == seq_idx.get_device() == positions.get_device() == dev
+            and block_table.is_contiguous() and seq_idx.is_contiguous() and positions.is_contiguous()):
+        for name, t, want in (("block_table", block_table, shape), ("seq_idx", seq_idx, (N,)), ("positions", positions, (N,))):
+            _whole(t, i32, want, dev, name)
+    return shape
 
 
 def kv_write_mx(k_new, v_new, block_table, seq_idx, positions, k_codes, k_scales, v_codes, v_scales, stream=None):
@@ -1033,10 +1048,12 @@ def kv_write_mx(k_new, v_new, block_table, seq_idx, positions, k_codes, k_scales
             return kv_write_mx(k_new, v_new, block_table, seq_idx, positions, k_codes, k_scales, v_codes, v_scales)
     P, hkv, page, d, kb, vb = _mx_pools(k_codes, k_scales, v_codes, v_scales, dev)
     stride = _kv_rows(k_new, v_new, dev, "k_new/v_new")
-    N = k_new.shape[0]
-    _need(k_new.shape[1:] == (hkv, d), "the cache is of other heads")
+    N, rows, width = k_new.shape
+    if rows != hkv or width != d:
+        raise ValueError("the cache is of other heads")
     B, maxp = _kv_places(block_table, seq_idx, positions, N, dev)
-    _sizes(N, B, maxp, page, P, hkv, d)
+    if max(N, B, maxp, page, P, hkv) > _MOST:
+        _sizes(N, B, maxp, page, P, hkv)
     _check(_load().uattn_kv_write_mx(k_new.data_ptr(), v_new.data_ptr(), stride, block_table.data_ptr(), seq_idx.data_ptr(),
                                      positions.data_ptr(), N, B, maxp, page, P, hkv, d, kb, vb, k_codes.data_ptr(),
                                      k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), _stream_on(dev)))
@@ -1059,11 +1076,17 @@ def kv_read_mx(k_codes, k_scales, v_codes, v_scales, block_table, seq_idx, posit
     P, hkv, page, d, kb, vb = _mx_pools(k_codes, k_scales, v_codes, v_scales, dev)
     N = positions.shape[0] if positions.dim() == 1 else -1
     B, maxp = _kv_places(block_table, seq_idx, positions, N, dev)
-    _sizes(N, B, maxp, page, P, hkv, d)
-    k_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if k_out is None else k_out
-    v_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if v_out is None else v_out
-    stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
-    _need(k_out.shape == (N, hkv, d), "k_out/v_out shape")
+    if max(N, B, maxp, page, P, hkv) > _MOST:
+        _sizes(N, B, maxp, page, P, hkv)
+    if k_out is None and v_out is None:
+        k_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16)
+        v_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16)
+        stride = hkv * d
+    else:
+        k_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if k_out is None else k_out
+        v_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if v_out is None else v_out
+        stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
+        _need(k_out.shape == (N, hkv, d), "k_out/v_out shape")
     _check(_load().uattn_kv_read_mx(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), kb, vb,
                                     block_table.data_ptr(), seq_idx.data_ptr(), positions.data_ptr(), N, B, maxp, page, P, hkv,
                                     d, k_out.data_ptr(), v_out.data_ptr(), stride, _stream_on(dev)))
@@ -1086,11 +1109,16 @@ def kv_round_mx(k, v, k_bits: int = 8, v_bits: int = 8, k_out=None, v_out=None, 
     _need(k_bits in (8, 4) and v_bits in (8, 4), "k_bits and v_bits are 8 or 4")
     stride = _kv_rows(k, v, dev, "k/v")
     N, hkv, d = shape = k.shape
-    _sizes(N, hkv, d)
-    k_out = torch.empty(shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=k.dtype, device=k.device) if v_out is None else v_out
-    out_stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
-    _need(k_out.shape == shape, "k_out/v_out shape")
+    if N > _MOST or hkv > _MOST or d > _MOST:
+        _sizes(N, hkv, d)
+    if k_out is None and v_out is None:
+        k_out, v_out = k.new_empty(shape), k.new_empty(shape)
+        out_stride = hkv * d
+    else:
+        k_out = k.new_empty(shape) if k_out is None else k_out
+        v_out = k.new_empty(shape) if v_out is None else v_out
+        out_stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
+        _need(k_out.shape == shape, "k_out/v_out shape")
     _check(_load().uattn_kv_round_mx(k.data_ptr(), v.data_ptr(), stride, N, hkv, d, k_bits, v_bits, k_out.data_ptr(),
                                      v_out.data_ptr(), out_stride, _stream_on(dev)))
     return k_out, v_out
@@ -1101,7 +1129,7 @@ def decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max
     """Token-wise paged decode against a cache in 8 or 4 bits (uattn_decode_mx).
 
     q [B,Hq,d] bf16; the cache as mx_cache makes it; block_table, seqlens, max_seqlen,
-    out and lse as for :func:`decode`.  ``workspace``: decode_workspace_bytes(...) bytes,
+    out and lse as for :func:`decode`.  ``workspace``: decode_mx_workspace_bytes(...) bytes,
     whatever they hold (a decode's own may serve); one is allocated when not given.
     """
     import torch
@@ -1111,40 +1139,53 @@ def decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max
         with there:
             return decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max_seqlen, softmax_scale, out,
                              return_lse, lse, workspace)
-    _need(q.dim() == 3, "q must be [B,Hq,d]")
-    B, hq, d = q.shape
-    bf16, i32 = torch.bfloat16, torch.int32
-    _whole(q, bf16, q.shape, dev, "q")
+    bf16, i32, shape, table = torch.bfloat16, torch.int32, q.shape, block_table.shape
+    if len(shape) != 3 or len(table) != 2:
+        raise ValueError("q must be [B,Hq,d], block_table [B,maxp]")
+    B, hq, d = shape
     P, hkv, page, d2, kb, vb = _mx_pools(k_codes, k_scales, v_codes, v_scales, dev)
-    _need(d2 == d, "head_dim mismatch")
-    _need(block_table.dim() == 2 and block_table.shape[0] == B, "block_table must be [B,maxp]")
-    _whole(block_table, i32, block_table.shape, dev, "block_table")
-    _whole(seqlens, i32, (B,), dev, "seqlens")
-    most = int(max_seqlen)
-    _sizes(B, block_table.shape[1], page, P, most, hq, hkv, d)
+    if d2 != d:
+        raise ValueError("head_dim mismatch")
+    maxp, most = table[1], int(max_seqlen)
+    if not (q.dtype is bf16 and block_table.dtype is seqlens.dtype is i32 and table[0] == B and seqlens.shape == (B,)
+            and block_table.get_device() == seqlens.get_device() == dev
+            and q.is_contiguous() and block_table.is_contiguous() and seqlens.is_contiguous()):
+        _whole(q, bf16, shape, dev, "q")
+        _whole(block_table, i32, (B, maxp), dev, "block_table")
+        _whole(seqlens, i32, (B,), dev, "seqlens")
+    if max(B, maxp, page, P, most, hq, hkv) > _MOST or most < -_MOST:
+        _sizes(B, maxp, page, P, most, hq, hkv)
     if out is None:
         out = torch.empty_like(q)
     else:
-        _whole(out, bf16, q.shape, dev, "out")
+        _whole(out, bf16, shape, dev, "out")
     if lse is not None:
         _whole(lse, torch.float32, (B, hq), dev, "lse")
     elif return_lse:
         lse = q.new_empty((B, hq), dtype=torch.float32)
-    need = _decode_need(B, most, hq, d)
-    if workspace is not None or need:
-        workspace = _workspace(workspace, need, q)
+    size = 0
+    if workspace is not None:
+        workspace = _workspace(workspace, 0, q)
+        size = workspace.numel() * workspace.element_size()
+    else:
+        size = _decode_mx_need(B, most, hq, hkv, d)
+        if size:
+            workspace = q.new_empty(size, dtype=torch.uint8)  # no initial contents needed
     _check(_load().uattn_decode_mx(q.data_ptr(), k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
-                                   v_scales.data_ptr(), kb, vb, block_table.data_ptr(), seqlens.data_ptr(), B,
-                                   block_table.shape[1], page, P, most, hq, hkv, d,
-                                   default_scale(d) if softmax_scale is None else softmax_scale, out.data_ptr(), _ptr(lse),
-                                   _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                   _stream_on(dev)))
+                                   v_scales.data_ptr(), kb, vb, block_table.data_ptr(), seqlens.data_ptr(), B, maxp, page, P,
+                                   most, hq, hkv, d, default_scale(d) if softmax_scale is None else softmax_scale,
+                                   out.data_ptr(), _ptr(lse), _ptr(workspace), size, _stream_on(dev)))
     return (out, lse) if lse is not None else out
 
 
+def decode_mx_workspace_bytes(batch: int, max_seqlen: int, num_q_heads: int, num_kv_heads: int, head_dim: int) -> int:
+    sizes = batch, max_seqlen, num_q_heads, num_kv_heads, head_dim
+    return _decode_mx_need(*sizes) if _fits(*sizes) else 0
+
+
 @functools.lru_cache(maxsize=256)
-def _decode_need(batch: int, max_seqlen: int, num_q_heads: int, head_dim: int) -> int:
-    return int(_load().uattn_decode_workspace_bytes(batch, max_seqlen, num_q_heads, head_dim))
+def _decode_mx_need(batch: int, max_seqlen: int, num_q_heads: int, num_kv_heads: int, head_dim: int) -> int:
+    return int(_load().uattn_decode_mx_workspace_bytes(batch, max_seqlen, num_q_heads, num_kv_heads, head_dim))
 
 
 def raw_call(name: str, *args) -> int:

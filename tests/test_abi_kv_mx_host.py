@@ -65,10 +65,22 @@ def test_round(lib, kw, code):
     (dict(hq=3), 1), (dict(hq=66), 2), (dict(scale=0.0), 1), (dict(scale=NAN), 1), (dict(scale=INF), 1), (dict(scale=-1.0), 1),
     (dict(most=-1), 1), (dict(most=0), 1), (dict(most=65), 1), (dict(most=(1 << 24) + 1, maxp=1 << 21), 2), (dict(np=0), 1),
     (dict(q=None), 1), (dict(q=P(24)), 1), (dict(out=None), 1), (dict(out=P(24)), 1), (dict(sl=None), 1),
-    (dict(most=300, maxp=32, ws=None), 3), (dict(most=300, maxp=32, wsb=1000), 3), (dict(most=300, maxp=32, ws=P(24)), 3),
+    (dict(most=2049, maxp=256, ws=None), 3), (dict(most=2049, maxp=256, wsb=1000), 3), (dict(most=2049, maxp=256, ws=P(24)), 3),
+    (dict(most=257, maxp=32, hq=34, d=128, ws=None), 3),
     (dict(B=0), 0), (dict(B=0, q=None, kc=None), 0), (dict(B=65536), 2),
 ])
 def test_decode(lib, kw, code):
     d = dict(q=P(16), kc=P(16), ks=P(16), vc=P(16), vs=P(16), kb=8, vb=4, bt=P(16), sl=P(16), B=2, maxp=4, page=16, np=8, most=64,
              hq=4, hkv=2, d=64, scale=0.125, out=P(16), lse=None, ws=P(16), wsb=1 << 24, stream=None)
     assert _call(lib.uattn_decode_mx, d, kw) == code
+
+
+def test_decode_workspace(lib):
+    """Nothing up to 2048 keys where a workgroup folds them; the bf16 decode's partials, without its counters, beyond."""
+    need, whole = lib.uattn_decode_mx_workspace_bytes, lib.uattn_decode_workspace_bytes
+    assert need(4, 2048, 32, 8, 128) == need(4, 2048, 34, 2, 64) == need(4, 256, 34, 2, 128) == need(4, 1, 1, 1, 64) == 0
+    for sizes in ((4, 2049, 32, 8, 128), (4, 257, 34, 2, 128), (300, 100000, 8, 8, 64)):
+        b, n, hq, _, d = sizes
+        assert need(*sizes) == whole(b, n, hq, d) - (4 * b * hq + 255) // 256 * 256
+    for bad in ((0, 4096, 8, 8, 64), (2, -1, 8, 8, 64), (2, 4096, 8, 3, 64), (2, 4096, 8, 0, 64)):
+        assert need(*bad) == 0

@@ -33,9 +33,9 @@ def ua(monkeypatch):
     monkeypatch.setattr(uattn, "_load", Library)
     monkeypatch.setattr(uattn, "_elsewhere", lambda device, stream: None)
     monkeypatch.setattr(uattn, "_stream_on", lambda device: 0)
-    uattn._decode_need.cache_clear()
+    uattn._decode_mx_need.cache_clear()
     yield uattn
-    uattn._decode_need.cache_clear()
+    uattn._decode_mx_need.cache_clear()
 
 
 def _cache(P=4, K=2, page=16, D=64, bits=(8, 4)):
@@ -80,7 +80,7 @@ def test_bits_follow_from_the_widths(ua, monkeypatch, bits):
             return lambda *args: seen.update({name: args}) or (16 if name.endswith("bytes") else 0)
 
     monkeypatch.setattr(ua, "_load", Library)
-    ua._decode_need.cache_clear()
+    ua._decode_mx_need.cache_clear()
     for D in (64, 128):
         for call in (_write(D=D, bits=bits), _read(D=D, bits=bits), _decode(D=D, bits=bits, page=32)):
             call(ua)

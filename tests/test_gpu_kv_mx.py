@@ -187,7 +187,7 @@ def both(ua, c, q, lens, most, table=None, scale=None):
     table = gu.dev_i32(c.table) if table is None else table
     out = torch.full_like(q, float("nan"))
     lse = torch.full(q.shape[:2], float("nan"), dtype=torch.float32, device="cuda")
-    need = ua.decode_workspace_bytes(q.shape[0], most, q.shape[1], q.shape[2])
+    need = ua.decode_mx_workspace_bytes(q.shape[0], most, q.shape[1], c.host[0].shape[1], q.shape[2])
     ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")    # any contents: NaN partials
     ua.decode_mx(q, *c.dev, table, lens, most, softmax_scale=scale, out=out, lse=lse, workspace=ws)
     want, wlse = ua.decode(q, c.kp, c.vp, table, lens, most, softmax_scale=scale, return_lse=True)
