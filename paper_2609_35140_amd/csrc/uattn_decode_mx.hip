@@ -522,10 +522,11 @@ __global__ __launch_bounds__(64) void decode_mx_merge_kernel(DecodeMxParams p) {
   const auto racc = buffer_rsrc(p.ws_acc + slot * D, nch * D * 4);
   const auto rml = buffer_rsrc(p.ws_ml + slot * 2, nch * 8);
   float x[2][kAhead];
+  // (the whole offset where the resource's bounds are checked: chunks past the last read 0)
   auto load = [&](int k0, float (&y)[kAhead]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      y[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(racc, d * 4, (k0 + i) * D * 4, 0));
+      y[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(racc, ((k0 + i) * D + d) * 4, 0, 0));
   };
   float M = 0.f, L = 0.f, A = 0.f;
   load(0, x[0]);
