@@ -605,8 +605,9 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
  * (E4M3 and E2M1 elements with E8M0 scales.)  e is the smallest whole number with
  * max|x| <= M * 2^e, -100 at least; the code is the nearest to x * 2^-e, ties to the
  * even code.  No element is clipped: each is off by at most 2^-4 (8 bits) or 2^-2 (4
- * bits) of its own size, or half a step at the block's bottom (2^(e-10) or 2^(e-2)).  A block whose largest magnitude is 2^127 or more, or that
- * holds an infinity or NaN, has the scale byte 255 and reads as NaN throughout.
+ * bits) of its own size, or half a step at the block's bottom (2^(e-10) or 2^(e-2)).  A
+ * block whose largest magnitude is 2^127 or more, or that holds an infinity or NaN, has
+ * the scale byte 255 and reads as NaN throughout.
  *
  * The cache is four arrays, codes and scale bytes of keys and of values:
  *
@@ -623,6 +624,8 @@ uattn_status uattn_logprob_backward(const void* logits, int64_t row_stride, cons
  * Indexed write of new keys and values into such a cache: uattn_kv_write with the rows
  * rounded as above.  k_new, v_new, token_stride, block_table, seq_idx, positions and
  * which tokens are not written: as there.  Every other row keeps its codes and scales.
+ * Two tokens mapping to one slot leave that row undefined (codes of one may meet scales
+ * of the other).
  */
 uattn_status uattn_kv_write_mx(const void* k_new, const void* v_new, int64_t token_stride, const int32_t* block_table,
                                const int32_t* seq_idx, const int32_t* positions, int32_t num_tokens, int32_t batch,
@@ -638,7 +641,8 @@ uattn_status uattn_kv_write_mx(const void* k_new, const void* v_new, int64_t tok
  *                        write (padding, or without a place in table or pool) gives zeros
  *   k_out, v_out         token rows of num_kv_heads * head_dim bf16 (written), out_stride
  *                        elements apart (>= num_kv_heads * head_dim, a multiple of 8);
- *                        16-byte aligned; what lies between the rows is left alone
+ *                        16-byte aligned, not one array; what lies between the rows is
+ *                        left alone
  */
 uattn_status uattn_kv_read_mx(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales,
                               int32_t k_bits, int32_t v_bits, const int32_t* block_table, const int32_t* seq_idx,

@@ -798,6 +798,7 @@ uattn_status uattn_kv_read_mx(const void* k_codes, const void* k_scales, const v
   if (!row_stride_ok(out_stride, num_kv_heads, head_dim)) return UATTN_EINVAL;
   if (num_tokens == 0) return UATTN_OK;
   if (!seq_idx || !positions || !k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return UATTN_EINVAL;
+  if (k_out == v_out) return UATTN_EINVAL;
   // without a table or a pool every token is one without a place
   const bool table = batch > 0 && max_pages_per_seq > 0;
   if (table && !block_table) return UATTN_EINVAL;

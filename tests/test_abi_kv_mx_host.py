@@ -41,10 +41,10 @@ def test_write(lib, kw, code):
     assert _call(lib.uattn_kv_write_mx, d, kw) == code
 
 
-@pytest.mark.parametrize("kw,code", SHARED + TOKENS)
+@pytest.mark.parametrize("kw,code", SHARED + TOKENS + [(dict(v=P(16)), 1)])
 def test_read(lib, kw, code):
     d = dict(kc=P(16), ks=P(16), vc=P(16), vs=P(16), kb=8, vb=4, bt=P(16), seq=P(16), pos=P(16), N=4, B=2, maxp=4, page=16, np=8,
-             hkv=2, d=64, k=P(16), v=P(16), st=128, stream=None)
+             hkv=2, d=64, k=P(16), v=P(32), st=128, stream=None)
     assert _call(lib.uattn_kv_read_mx, d, kw) == code
 
 
