@@ -53,6 +53,7 @@ struct DecodeMxParams {
   float* ws_acc;  // [batch][Hq][nslot][D]
   float* ws_ml;   // [batch][Hq][nslot][2]
   int batch, hq, hkv, group, maxp, page_size, page_shift, num_pages, max_seqlen, nchunk_max, nslot;
+  int stride;     // kChunks, kWalk: waves of an (entry, kv head)
   int first;      // workgroups of the launches before this one
   float c;
 };
@@ -153,20 +154,22 @@ __device__ __forceinline__ void settle(f32x4 (&s)[NB][kKeyBlocks]) {
 //   kChunks  a workgroup is one wave and takes one chunk of an (entry, kv head); fp32
 //            partials go to the workspace for decode_mx_merge_kernel (entries of one chunk
 //            are finished)
+//   kWalk    the same, but a wave takes every stride-th chunk
 //   kFused   a workgroup takes all chunks, at most kTeamWaves, of an (entry, kv head), one
 //            to a wave, and folds them in LDS behind one barrier
 //   kTeam    a workgroup takes all chunks of an (entry, kv head), its waves in turn; a
 //            wave adds its chunk to one state in LDS when the chunks before are in it
-enum class Split { kChunks, kFused, kTeam };
+enum class Split { kChunks, kWalk, kFused, kTeam };
 constexpr int kTeamWaves = 8;  // of a kFused workgroup, at most
 constexpr int kTurnWaves = 4;  // of a kTeam workgroup: two to a CU
+constexpr int64_t kMostWaves = 32768;  // of one wave each, where (entry, kv head) pairs alone are not more
 
 // kLoad: cache policy of the loads of codes (0, or kStreamed).
 constexpr int kStreamed = 2;   // the nt bit of the buffer instructions' cache-policy operand
 constexpr int kCoherent = 16;  // the sc1 bit: stores to the device-coherent level
 
 template <int D, int NB, int KB, int VB, Split kSplit, int kLoad>
-__global__ __launch_bounds__(64 * (kSplit == Split::kChunks ? 1 : kSplit == Split::kFused ? kTeamWaves : kTurnWaves)) void decode_mx_kernel(
+__global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::kWalk ? 1 : kSplit == Split::kFused ? kTeamWaves : kTurnWaves)) void decode_mx_kernel(
     DecodeMxParams p, const int32_t* __restrict__ seqlens, const int32_t* __restrict__ block_table) {
   using TL = TileLayout<D>;
   using RK = MxRow<D, KB>;
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks ? 1 : kSplit == Spli
   constexpr int KS = D / 32;   // K steps of the score product
   constexpr int NDB = D / 16;  // d blocks of the output
   constexpr int kPieces = D / 4;  // 16-byte pieces of a head's partial
-  constexpr bool kFused = kSplit == Split::kFused, kTeam = kSplit == Split::kTeam;
+  constexpr bool kFused = kSplit == Split::kFused, kTeam = kSplit == Split::kTeam, kChunks = !kFused && !kTeam;
   constexpr int kWaves = kFused ? kTeamWaves : kTeam ? kTurnWaves : 1;
   // the next tile's codes have registers of their own where there are enough
   constexpr bool kTwo = !kTeam || KB + VB < 16;
@@ -197,12 +200,12 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks ? 1 : kSplit == Spli
   const int u = p.first + blockIdx.x;
   const int kvh = u % p.hkv;
   int chunk = wave, b = u / p.hkv;
-  if constexpr (kSplit == Split::kChunks) {
-    chunk = b % p.nchunk_max;
-    b /= p.nchunk_max;
+  if constexpr (kChunks) {
+    chunk = b % p.stride;
+    b /= p.stride;
   }
   const int n = min(seqlens[b], p.max_seqlen);
-  if (kSplit == Split::kChunks ? chunk * kChunkKeys >= n : n < 1) return;
+  if (kChunks ? chunk * kChunkKeys >= n : n < 1) return;
   if constexpr (kTeam) {
     if (threadIdx.x == 0) turn = 0;
     __syncthreads();
@@ -444,31 +447,43 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks ? 1 : kSplit == Spli
     return;
   }
 
-  if (!kFused || chunk < nch) {
+  auto only = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) finish(nb, m[nb], lsum[nb][0]);
+  };
+  if constexpr (kChunks) {
+    const int64_t row = static_cast<int64_t>(b) * p.hq + head0;
+#pragma unroll 1
+    for (;;) {
+      load_tile(codes[0], chunk, pages, 0);
+      chunk_step(chunk, chunk, pages);
+      if (nch == 1) return only();
+      // heads past the group's fall outside the resource and store nothing
+      const auto racc = buffer_rsrc(p.ws_acc + row * p.nslot * D, p.group * p.nslot * D * 4);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int gi = kQCols * nb + col;
+        const int off = ((gi * p.nslot + chunk) * D + 4 * g) * 4;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[nb][db]), racc, off + 64 * db, 0, kCoherent);
+        if (g == 0 && gi < p.group)
+          *reinterpret_cast<float2*>(p.ws_ml + ((row + gi) * p.nslot + chunk) * 2) = float2{m[nb], lsum[nb][0]};
+      }
+      chunk += p.stride;
+      if (kSplit == Split::kChunks || chunk >= nch) return;
+      pages = load_pages(chunk);
+    }
+  }
+  if (chunk < nch) {
     load_tile(codes[0], chunk, pages, 0);
     chunk_step(chunk, chunk, pages);
   }
   if (nch == 1) {
-    if (chunk == 0)
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) finish(nb, m[nb], lsum[nb][0]);
+    if (chunk == 0) only();
     return;
   }
-  if constexpr (kSplit == Split::kChunks) {
-    // heads past the group's fall outside the resource and store nothing
-    const int64_t row = static_cast<int64_t>(b) * p.hq + head0;
-    const auto racc = buffer_rsrc(p.ws_acc + row * p.nslot * D, p.group * p.nslot * D * 4);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int gi = kQCols * nb + col;
-      const int off = ((gi * p.nslot + chunk) * D + 4 * g) * 4;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[nb][db]), racc, off + 64 * db, 0, kCoherent);
-      if (g == 0 && gi < p.group)
-        *reinterpret_cast<float2*>(p.ws_ml + ((row + gi) * p.nslot + chunk) * 2) = float2{m[nb], lsum[nb][0]};
-    }
-  } else if constexpr (kFused) {
+  if constexpr (kFused) {
     if (chunk < nch) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
@@ -602,9 +617,14 @@ hipError_t launch(DecodeMxParams p, int num_cus, hipStream_t stream) {
   // them holds (256 MB): 8 x 32K keys 73 -> 68 us, 64 of 4000-8000, d = 64, 4 bits 56 -> 53; 10
   // of 1500-12000, 136/8 heads (64 MB, bound 104) 28 -> 31.
   const int64_t bytes = pairs * p.max_seqlen * (MxRow<D, KB>::kBytes + MxRow<D, VB>::kBytes + 2 * MxRow<D, KB>::kScales);
-  const hipError_t e = bytes > (int64_t{128} << 20)
-                           ? run(decode_mx_kernel<D, NB, KB, VB, Split::kChunks, kStreamed>, pairs * p.nchunk_max, 1)
-                           : run(decode_mx_kernel<D, NB, KB, VB, Split::kChunks, 0>, pairs * p.nchunk_max, 1);
+  // A wave to each chunk up to 32768 waves, as those without keys cost too: 64 entries of
+  // 500-1000 keys, 32/8 heads, 4 bits under a bound of 128K keys 68 us so, 26 with a walk.
+  const int64_t most = pairs < kMostWaves ? kMostWaves / pairs : 1;
+  p.stride = p.nchunk_max < most ? p.nchunk_max : static_cast<int>(most);
+  const hipError_t e = p.stride < p.nchunk_max ? run(decode_mx_kernel<D, NB, KB, VB, Split::kWalk, kStreamed>, pairs * p.stride, 1)
+                       : bytes > (int64_t{128} << 20)
+                           ? run(decode_mx_kernel<D, NB, KB, VB, Split::kChunks, kStreamed>, pairs * p.stride, 1)
+                           : run(decode_mx_kernel<D, NB, KB, VB, Split::kChunks, 0>, pairs * p.stride, 1);
   if (e != hipSuccess || p.nchunk_max == 1) return e;
   return launch_parts(static_cast<int64_t>(p.batch) * p.hq * (D / 64), 64, [&](int first, unsigned n) {
     p.first = first;
@@ -642,7 +662,7 @@ hipError_t launch_decode_mx(const DecodeLaunch& a, const MxCache& cache, hipStre
   p.max_seqlen = a.max_seqlen;
   p.nchunk_max = a.nchunk_max;
   p.nslot = static_cast<int>(decode_slots(a.nchunk_max));
-  p.first = 0;
+  p.first = p.stride = 0;
   p.c = a.c;
   using std::integral_constant;
   auto pick = [&](auto d, auto nb, auto kb, auto vb) {

@@ -261,6 +261,14 @@ def test_decode_many_long_sequences(ua, bits, hq, hkv, d):
 
 
 @pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("hq,d", [(4, 128), (34, 128), (8, 64), (40, 64)])
+def test_decode_more_chunks_than_waves(ua, bits, hq, d):
+    """Six hundred pairs of sequence and kv head, 67 chunks: some sequences have more chunks than a pair has waves."""
+    lens = [17000, 1, 0, 54 * 256, 54 * 256 + 1, 55 * 256, 15000, 256, 257, -3] + list(inputs.rng(641, d).integers(1, 900, 290))
+    _many(ua, lens, hq, 2, d, bits, 90)
+
+
+@pytest.mark.parametrize("bits", BITS)
 @pytest.mark.parametrize("hq,hkv,d,long", [(4, 2, 128, 2048), (34, 2, 64, 1500), (34, 2, 128, 1500), (16, 1, 64, 300), (8, 1, 128, 900)])
 def test_decode_few_chunks(ua, bits, hq, hkv, d, long):
     """Up to eight chunks, entries of fewer among them."""
