@@ -135,6 +135,80 @@ def test_write_and_read(ua, bits, N, hkv, d, page):
     assert bool((wide[:, hkv] == 5.0).all())
 
 
+def _equal(got, want):
+    """Equal bf16 numbers on the device; any NaN stands for any other."""
+    import torch
+    nan = torch.isnan(want)
+    return bool(torch.equal(torch.isnan(got), nan) and torch.equal(got.view(torch.int16)[~nan], want.view(torch.int16)[~nan]))
+
+
+@pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("N,hkv,d", [(8301, 8, 128), (33331, 8, 128), (100003, 6, 64), (262145, 1, 128)])
+def test_rows_larger_than_the_caches(ua, bits, N, hkv, d):
+    """Rows of 17 to 77 MB (past the caches in some calls, in others not): those of a small call, repeated; places in any order,
+    some tokens without one."""
+    import torch
+    k, v = gu.dev(rows_of((1009, hkv, d), 5)), gu.dev(rows_of((1009, hkv, d), 6))
+    small = ua.kv_round_mx(k, v, *bits)
+    assert same_values(gu.host_bits(small[0]), oracle.mx_round(gu.host_bits(k), bits[0]))
+    assert same_values(gu.host_bits(small[1]), oracle.mx_round(gu.host_bits(v), bits[1]))
+    at = torch.arange(N, device="cuda") % 1009
+    k, v = k[at], v[at]
+    got = ua.kv_round_mx(k, v, *bits)
+    assert _equal(got[0], small[0][at]) and _equal(got[1], small[1][at])
+    g = inputs.rng(602, N)
+    maxp = N // 64 + 1
+    table = g.permutation(maxp).astype(np.int32)[None]
+    pos = g.permutation(maxp * 64)[:N].astype(np.int32)
+    pos[g.integers(0, N, 50)] = -1
+    pos[N - 1] = maxp * 64
+    places = gu.dev_i32(table), torch.zeros(N, dtype=torch.int32, device="cuda"), gu.dev_i32(pos)
+    cache = ua.mx_cache(maxp, hkv, 64, d, *bits)
+    ua.kv_write_mx(k, v, *places, *cache)
+    back = ua.kv_read_mx(*cache, *places)
+    there = torch.from_numpy((pos >= 0) & (pos < maxp * 64)).cuda()[:, None, None]
+    for b, w in zip(back, got):
+        assert _equal(b, torch.where(there, w, 0))
+    # in place
+    ua.kv_round_mx(k, v, *bits, k_out=k, v_out=v)
+    assert _equal(k, got[0]) and _equal(v, got[1])
+
+
+def test_past_32_bits(ua):
+    """A pool of 4.6 GB of codes and rows 4.4 GB long: offsets that have no 32-bit number."""
+    import torch
+    P, hkv, page, d, N = 70001, 8, 64, 128, 2200003
+    k = torch.empty((N, hkv, d), dtype=torch.bfloat16, device="cuda")
+    tail = gu.dev(rows_of((2048, hkv, d), 7, special=False))
+    for lo in (0, N - 2048):
+        k[lo:lo + 2048] = tail
+    kr, vr = ua.kv_round_mx(k, k, 8, 4)
+    wk, wv = ua.kv_round_mx(tail, tail, 8, 4)
+    for lo in (0, N - 2048):
+        assert torch.equal(kr[lo:lo + 2048], wk) and torch.equal(vr[lo:lo + 2048], wv)
+    del kr, vr
+    big, small = ua.mx_cache(P, hkv, page, d, 8, 4), ua.mx_cache(32, hkv, page, d, 8, 4)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    high = torch.arange(P - 32, P, **i32)[None]
+    low = torch.arange(32, **i32)[None]
+    # padding for all rows but the last ones, which go to the last pages
+    pos = torch.full((N,), -1, **i32)
+    pos[N - 2048:] = torch.arange(2048, **i32)
+    zero = torch.zeros(N, **i32)
+    ua.kv_write_mx(k, k, high, zero, pos, *big)
+    ua.kv_write_mx(tail, tail, low, zero[:2048], pos[N - 2048:], *small)
+    for b, s in zip(big, small):
+        assert torch.equal(b[P - 32:], s) and not bool(b[:P - 32].any())
+    rk, rv = ua.kv_read_mx(*big, high, zero, pos, k_out=k, v_out=torch.empty_like(k))
+    assert torch.equal(rk[N - 2048:], wk) and torch.equal(rv[N - 2048:], wv) and not bool(rk[:N - 2048].any())
+    q = gu.dev(inputs.normal_bf16((1, 16, d), 1.0, 630))
+    n = torch.tensor([2048], **i32)
+    assert torch.equal(ua.decode_mx(q, *big, high, n, 2048), ua.decode_mx(q, *small, low, n, 2048))
+    wide = torch.full((1, 64), -1, **i32)
+    wide[:, :32] = high
+    assert torch.equal(ua.decode_mx(q, *big, wide, n, 4096), ua.decode_mx(q, *small, low, n, 2048))
+
+
 def test_read_without_a_table(ua):
     """No sequences, no table columns, no pages: zeros."""
     import torch
