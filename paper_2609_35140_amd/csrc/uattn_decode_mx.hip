@@ -168,8 +168,16 @@ constexpr int64_t kMostWaves = 32768;  // of one wave each, where (entry, kv hea
 constexpr int kStreamed = 2;   // the nt bit of the buffer instructions' cache-policy operand
 constexpr int kCoherent = 16;  // the sc1 bit: stores to the device-coherent level
 
+// Two blocks of heads at d = 128 take all registers of a SIMD; in 4 bits half of them
+// will do, with the queries in LDS and the next tile's codes in this tile's registers.
+// 17/1 heads of 10 x 1500-12000 keys 28.9 -> 25.6 us, 32/1 of 16 x 4000-8000
+// 30.2 -> 26.7; with 8 bits on either side registers spill (31.9 -> 34.0).
+template <int D, int NB, int KB, int VB>
+constexpr bool kHalfSimd = NB == 2 && D == 128 && KB + VB == 8;
+
 template <int D, int NB, int KB, int VB, Split kSplit, int kLoad>
-__global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::kWalk ? 1 : kSplit == Split::kFused ? kTeamWaves : kTurnWaves)) void decode_mx_kernel(
+__global__ __launch_bounds__(64 * (kSplit == Split::kFused ? kTeamWaves : kSplit == Split::kTeam ? kTurnWaves : 1),
+                             (kHalfSimd<D, NB, KB, VB> ? 2 : 1)) void decode_mx_kernel(
     DecodeMxParams p, const int32_t* __restrict__ seqlens, const int32_t* __restrict__ block_table) {
   using TL = TileLayout<D>;
   using RK = MxRow<D, KB>;
@@ -179,13 +187,17 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::
   constexpr int kPieces = D / 4;  // 16-byte pieces of a head's partial
   constexpr bool kFused = kSplit == Split::kFused, kTeam = kSplit == Split::kTeam, kChunks = !kFused && !kTeam;
   constexpr int kWaves = kFused ? kTeamWaves : kTeam ? kTurnWaves : 1;
-  // the next tile's codes have registers of their own where there are enough
-  constexpr bool kTwo = !kTeam || KB + VB < 16;
+  // The next tile's codes have registers of their own where there are enough.  kTeam, 256
+  // entries, 32/8 heads of 128: 4000 keys, keys in 4 bits, values in 8 320 us with, 307
+  // without; keys in 8, values in 4 271 and 281.  Of 64, 500-8000 keys, 8 bits: 226 and 237.
+  constexpr bool kQueriesInLds = kHalfSimd<D, NB, KB, VB>;
+  constexpr bool kTwo = !kQueriesInLds && !(kTeam && D == 128 && VB == 8);
   // per wave: 32 keys' values on their way to the products; then (kFused) its partial
   // [NB][16][D] fp32.  Rows of partials and of the state below: 16-byte pieces,
   // XOR-swizzled by the head.
   static_assert(32 * sizeof(__bf16) == kQCols * sizeof(float), "a partial of 16 heads takes 32 keys' room");
   __shared__ __attribute__((aligned(1024))) __bf16 room[kWaves][(kFused ? NB : 1) * 32 * D];
+  __shared__ bf16x8 queries[kQueriesInLds ? NB * kQCols * KS * 4 : 1];  // rows' pieces swizzled by the head
   __shared__ float2 ml[kFused ? kWaves : 1][NB * kQCols];
   // kTeam: the fold so far and how many chunks it holds
   __shared__ __attribute__((aligned(16))) f32x4 state[kTeam ? NB * kQCols * kPieces : 1];
@@ -232,6 +244,19 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::
         qf[nb][st] = __builtin_bit_cast(
             bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, (nb * kQCols + col) * D * 2 + 16 * g + 64 * st, 0, 0));
   }
+
+  if constexpr (kQueriesInLds) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int st = 0; st < KS; ++st) queries[(nb * kQCols + col) * (4 * KS) + ((4 * st + g) ^ col)] = qf[nb][st];
+  }
+  auto query = [&](int nb, int st) __attribute__((always_inline)) {
+    if constexpr (kQueriesInLds)
+      return queries[(nb * kQCols + col) * (4 * KS) + ((4 * st + g) ^ col)];
+    else
+      return qf[nb][st];
+  };
 
   // Codes of 16-key block kb of tile t of chunk ch.  Blocks past the context, on a page
   // outside the pool or past the table read as zeros (codes 0, scale byte 0) without
@@ -308,7 +333,7 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::
       for (int nb = 0; nb < NB; ++nb) {
         f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int st = 0; st < KS; ++st) r = mfma16(a[st], qf[nb][st], r);
+        for (int st = 0; st < KS; ++st) r = mfma16(a[st], query(nb, st), r);
         s[nb][kb] = r;
       }
     }
@@ -317,7 +342,8 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::
       // the registers of these keys take the next tile's
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < kKeyBlocks; ++kb) load_k(x, place(ch_next, next_pages, t_next, kb), kb);
+      for (int kb = 0; kb < kKeyBlocks; ++kb)
+        if (kTeam || t_next > 0) load_k(x, place(ch_next, next_pages, t_next, kb), kb);
       __builtin_amdgcn_sched_barrier(0);
     }
     float alpha[NB];
@@ -350,7 +376,8 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kChunks || kSplit == Split::
       if constexpr (!kTwo) {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 2 * st; kb < 2 * st + 2; ++kb) load_v(x, place(ch_next, next_pages, t_next, kb), kb);
+        for (int kb = 2 * st; kb < 2 * st + 2; ++kb)
+          if (kTeam || t_next > 0) load_v(x, place(ch_next, next_pages, t_next, kb), kb);
         __builtin_amdgcn_sched_barrier(0);
       }
       // acc <- acc + V^T P^T and lsum <- lsum + 1^T P^T over them: step st of pv_tile
@@ -599,8 +626,8 @@ hipError_t launch(DecodeMxParams p, int num_cus, hipStream_t stream) {
       hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * waves), 0, stream, p, p.seqlens, p.bt);
     });
   };
-  // Registers for two blocks of heads at d = 128 are those of one wave to a SIMD, which
-  // larger workgroups cannot have: chunks alone there.
+  // Two blocks of heads at d = 128 have no registers (8 bits) or no room in LDS (4) for
+  // workgroups of more waves: chunks alone there.
   if constexpr (NB == 1 || D == 64) {
     // Up to kTeamWaves chunks: one launch, nothing through memory.  A step of 700 keys,
     // 32/8 heads, 8 bits 10.7 us with a merge, 9.1 so; 64 entries of 300-2000 keys, 32/8
