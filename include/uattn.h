@@ -683,9 +683,11 @@ size_t uattn_decode_mx_workspace_bytes(int32_t batch, int32_t max_seqlen, int32_
  *   workspace   device scratch of at least uattn_decode_mx_workspace_bytes(batch,
  *               max_seqlen, num_q_heads, num_kv_heads, head_dim) bytes, 16-byte aligned
  *               (may be NULL when that is 0).  No initial contents are needed.  The
- *               partials go at its end: one that is large enough for uattn_decode with
- *               these sizes keeps that call's counters as they are, so that the two may
- *               share it.  Calls that share a workspace must be ordered on one stream.
+ *               partials go at its end and nothing else is written: uattn_decode may
+ *               share it, and keeps its C bytes of counters as they are where the
+ *               workspace has C bytes more than this call needs; where it has fewer
+ *               they are zeroed again before that call.  Calls that share a workspace
+ *               must be ordered on one stream.
  */
 uattn_status uattn_decode_mx(const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
                              const void* v_scales, int32_t k_bits, int32_t v_bits, const int32_t* block_table,

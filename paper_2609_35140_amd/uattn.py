@@ -1130,7 +1130,10 @@ def decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max
 
     q [B,Hq,d] bf16; the cache as mx_cache makes it; block_table, seqlens, max_seqlen,
     out and lse as for :func:`decode`.  ``workspace``: decode_mx_workspace_bytes(...) bytes,
-    whatever they hold (a decode's own may serve); one is allocated when not given.
+    whatever they hold; one is allocated when not given.  A decode's own may serve: which of its
+    counters this call leaves zero is recorded, and :func:`decode` clears the others.  A graph's
+    replays record nothing: one that they share holds these bytes and the decode's counters
+    (counter_bytes) side by side.
     """
     import torch
     dev = _gpu_of(q, "q")
@@ -1167,6 +1170,10 @@ def decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max
     if workspace is not None:
         workspace = _workspace(workspace, 0, q)
         size = workspace.numel() * workspace.element_size()
+        known = getattr(workspace, "_uattn_zero_prefix", 0)
+        if known and _decode_mx_need(B, most, hq, hkv, d):
+            # counters of a decode that the partials reach are no longer known to be zero
+            workspace._uattn_zero_prefix = max(0, min(known, _partials_start(size, B, most, hq, d)))
     else:
         size = _decode_mx_need(B, most, hq, hkv, d)
         if size:
