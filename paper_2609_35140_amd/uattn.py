@@ -1020,6 +1020,22 @@ def _kv_rows(k, v, dev, names):
     return stride[0]
 
 
+def _kv_outputs(k_out, v_out, shape, like, dev):
+    """(k_out, v_out, elements from token to token) of outputs of this shape, made where they are not given (beside a given
+    one: alike)."""
+    import torch
+    n, hkv, d = shape
+    if k_out is None and v_out is None:
+        return like.new_empty(shape, dtype=torch.bfloat16), like.new_empty(shape, dtype=torch.bfloat16), hkv * d
+    given = v_out if k_out is None else k_out
+    _need(given.shape == shape and (v_out is None or v_out.shape == shape), "k_out/v_out shape")
+    stride = _kv_rows(given, given if v_out is None else v_out, dev, "k_out/v_out")
+    if k_out is None or v_out is None:
+        made = torch.empty_strided(shape, (stride, d, 1), dtype=torch.bfloat16, device=given.device)
+        k_out, v_out = (made, v_out) if k_out is None else (k_out, made)
+    return k_out, v_out, stride
+
+
 def _kv_places(block_table, seq_idx, positions, N, dev):
     """(B, maxp) of the indices that say where N tokens live."""
     import torch
@@ -1065,9 +1081,8 @@ def kv_read_mx(k_codes, k_scales, v_codes, v_scales, block_table, seq_idx, posit
 
       seq_idx, positions [N] int32: row n is the token at positions[n] of sequence seq_idx[n]
       (zeros for padding, position < 0, and tokens without a place)
-    Returns (k, v) [N, Hkv, d] bf16.
+    Returns (k, v) [N, Hkv, d] bf16 (of k_out and v_out one may be given alone).
     """
-    import torch
     dev = _gpu_of(k_codes, "k_codes")
     there = _elsewhere(dev, stream)
     if there is not None:
@@ -1078,15 +1093,7 @@ def kv_read_mx(k_codes, k_scales, v_codes, v_scales, block_table, seq_idx, posit
     B, maxp = _kv_places(block_table, seq_idx, positions, N, dev)
     if max(N, B, maxp, page, P, hkv) > _MOST:
         _sizes(N, B, maxp, page, P, hkv)
-    if k_out is None and v_out is None:
-        k_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16)
-        v_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16)
-        stride = hkv * d
-    else:
-        k_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if k_out is None else k_out
-        v_out = k_codes.new_empty((N, hkv, d), dtype=torch.bfloat16) if v_out is None else v_out
-        stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
-        _need(k_out.shape == (N, hkv, d), "k_out/v_out shape")
+    k_out, v_out, stride = _kv_outputs(k_out, v_out, (N, hkv, d), k_codes, dev)
     _check(_load().uattn_kv_read_mx(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), kb, vb,
                                     block_table.data_ptr(), seq_idx.data_ptr(), positions.data_ptr(), N, B, maxp, page, P, hkv,
                                     d, k_out.data_ptr(), v_out.data_ptr(), stride, _stream_on(dev)))
@@ -1097,10 +1104,9 @@ def kv_round_mx(k, v, k_bits: int = 8, v_bits: int = 8, k_out=None, v_out=None, 
     """The values that a cache in k_bits and v_bits would hold for packed rows (uattn_kv_round_mx).
 
       k, v [N, Hkv, d] bf16 (token rows may be strided).  Returns (k_out, v_out), which
-      may be k and v themselves (in place).  The gradient of the rounded rows passes to
-      the rows as it is.
+      may be k and v themselves (in place), or one given alone.  The gradient of the
+      rounded rows passes to the rows as it is.
     """
-    import torch
     dev = _gpu_of(k, "k")
     there = _elsewhere(dev, stream)
     if there is not None:
@@ -1111,14 +1117,7 @@ def kv_round_mx(k, v, k_bits: int = 8, v_bits: int = 8, k_out=None, v_out=None, 
     N, hkv, d = shape = k.shape
     if N > _MOST or hkv > _MOST or d > _MOST:
         _sizes(N, hkv, d)
-    if k_out is None and v_out is None:
-        k_out, v_out = k.new_empty(shape), k.new_empty(shape)
-        out_stride = hkv * d
-    else:
-        k_out = k.new_empty(shape) if k_out is None else k_out
-        v_out = k.new_empty(shape) if v_out is None else v_out
-        out_stride = _kv_rows(k_out, v_out, dev, "k_out/v_out")
-        _need(k_out.shape == shape, "k_out/v_out shape")
+    k_out, v_out, out_stride = _kv_outputs(k_out, v_out, shape, k, dev)
     _check(_load().uattn_kv_round_mx(k.data_ptr(), v.data_ptr(), stride, N, hkv, d, k_bits, v_bits, k_out.data_ptr(),
                                      v_out.data_ptr(), out_stride, _stream_on(dev)))
     return k_out, v_out
