@@ -28,6 +28,7 @@ that skips the body.
 """
 from __future__ import annotations
 
+import functools
 import os
 import re
 import subprocess
@@ -213,6 +214,7 @@ def scan(text: str):
     return findings
 
 
+@functools.lru_cache(maxsize=None)
 def assembly(src: str) -> str:
     """gfx950 device assembly of one kernel source, built with the library's flags."""
     with tempfile.TemporaryDirectory() as tmp:
@@ -224,6 +226,15 @@ def assembly(src: str) -> str:
             raise RuntimeError(f"assembly of {src} failed:\n{res.stderr[-4000:]}")
         with open(out) as fh:
             return fh.read()
+
+
+def resources(text: str):
+    """{kernel: {"vgpr_spill_count": .., "private_segment_fixed_size": .. (bytes of scratch a lane), ..}} of an assembly text."""
+    found = {}
+    for part in re.split(r"^  - (?=\.agpr_count:)", text, flags=re.M)[1:]:
+        fields = dict(re.findall(r"^ *\.(\w+): +(\S+)$", part, flags=re.M))
+        found[fields["name"]] = {k: int(v) for k, v in fields.items() if v.isdigit()}
+    return found
 
 
 def check(sources=SOURCES, scans=(scan, scan_matrix)):

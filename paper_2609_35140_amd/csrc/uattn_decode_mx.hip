@@ -487,9 +487,12 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kFused ? kTeamWaves : kSplit
       if (nch == 1) return only();
       // heads past the group's fall outside the resource and store nothing
       const auto racc = buffer_rsrc(p.ws_acc + row * p.nslot * D, p.group * p.nslot * D * 4);
+      int head = col;
+      // (the addresses of these stores are formed anew: kept over the walk they cost a register too many)
+      if constexpr (kSplit == Split::kWalk && kQueriesInLds) asm volatile("" : "+v"(head));
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const int gi = kQCols * nb + col;
+        const int gi = kQCols * nb + head;
         const int off = ((gi * p.nslot + chunk) * D + 4 * g) * 4;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
