@@ -12,12 +12,12 @@
 // with a >= 2^127 (rounding up could leave bf16's range), an infinity or a NaN gets
 // the scale byte 255, which reads as NaN in every element.
 //
-// Every code times every scale that a write makes is a bf16 number, and the gfx950
-// conversions below give exactly it (and exactly the nearest code): checked for all
-// 256 codes with all scale bytes from 3 to 246, and for all bf16 values.  So reading
-// back rounds nothing, and attention over a cache has the bits of attention over
-// those bf16 values.  Below e = -100 (elements under 2^-109) nothing is kept: the
-// clamp keeps every value a normal number.
+// Every code times every scale that a write makes (bytes 27 to 246 in 8 bits, 27 to 252
+// in 4) is a bf16 number, and the gfx950 conversions below give exactly it (and exactly
+// the nearest code): tested for all codes with all of these bytes, and for all bf16
+// values.  So reading back rounds nothing, and attention over a cache has the bits of
+// attention over those bf16 values.  The floor of e keeps every value a normal number:
+// the smallest is 2^-109 in 8 bits and 2^-101 in 4, and half of it and less becomes zero.
 #pragma once
 
 #include "uattn_numerics.h"
