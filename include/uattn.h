@@ -634,8 +634,10 @@ uattn_status uattn_kv_write_mx(const void* k_new, const void* v_new, int64_t tok
                                void* v_codes, void* v_scales, void* stream);
 
 /*
- * Rows of such a cache as bf16, packed (what uattn_prefill reads): the keys and values
- * of the token at positions[n] of sequence seq_idx[n] become row n.
+ * Rows of such a cache as bf16, packed as uattn_prefill and uattn_kv_write take keys and
+ * values: those of the token at positions[n] of sequence seq_idx[n] become row n.
+ * uattn_prefill has a query for every key, so over rows read back it needs the queries
+ * of all of them; single queries attend to the cache itself (uattn_decode_mx).
  *
  *   seq_idx, positions   [num_tokens] int32.  A token that uattn_kv_write_mx would not
  *                        write (padding, or without a place in table or pool) gives zeros

@@ -1077,7 +1077,8 @@ def kv_write_mx(k_new, v_new, block_table, seq_idx, positions, k_codes, k_scales
 
 
 def kv_read_mx(k_codes, k_scales, v_codes, v_scales, block_table, seq_idx, positions, k_out=None, v_out=None, stream=None):
-    """Rows of a cache in 8 or 4 bits as bf16 (uattn_kv_read_mx).
+    """Rows of a cache in 8 or 4 bits as bf16, packed (uattn_kv_read_mx).  A prefill over them takes
+    the queries of all rows; single queries attend to the cache itself (decode_mx).
 
       seq_idx, positions [N] int32: row n is the token at positions[n] of sequence seq_idx[n]
       (zeros for padding, position < 0, and tokens without a place)
