@@ -19,18 +19,22 @@
 //      the transposing read of the P V product expects, 32 keys at a time (a wave's own
 //      8 KB, in order: no barrier).
 //
-// What bounds it: memory.  Timing copies of 8 x 32K keys, 64/8 heads, 4 bits (285 MB of
-// codes and scales, 73 us with its merge): without arithmetic and partials 61, without
-// the partials alone 66, without V's part of the arithmetic 71.  The partials (34 MB)
-// are what costs: mixed into a read stream they take several times their share of the
-// bytes, in whatever order, width or policy they are stored (as [chunk][head][d] in whole
-// lines: no change; past the caches: no change; device-coherent: 1-3% less, kept).
-// So where many (entry, kv head) pairs are there, a workgroup keeps a pair to itself and
-// nothing is stored (Split, below).  Codes are read past the caches where there are more
-// than these hold (73 -> 68 us; a step of 64 MB that the caches hold 28 -> 31).  A walk of
-// persistent waves, the next item's codes on their way while one is computed, was no
-// faster than one wave an item (78 against 73), nor were three waves to a SIMD, for whose
-// registers the next tile's codes come later (78 against 77).
+// The weights are rounded to bf16 for the P V product and its normaliser, as uattn_decode
+// does (2^-8 of each; without this the two would have other bits): rows are off by 0.0022
+// of their size against 64 bits, 0.0017 with weights in 32 bits.
+//
+// What bounds it: memory.  8 x 32K keys, 64/8 heads, 4 bits (285 MB of codes and scales)
+// take 65 us.  Timing copies: without the merge's launch 57, without partials at all 51,
+// without the conversion of V too 47, loads alone 44 (6.5 TB/s).  In 8 bits (554 MB) 113,
+// 105, 89, 88 and 88.  The partials (34 MB) are what costs: mixed into a read stream they
+// take several times their share of the bytes, in whatever order, width or policy they are
+// stored (as [chunk][head][d] in whole lines: no change; past the caches: no change;
+// device-coherent: 1-3% less, kept).  So where many (entry, kv head) pairs are there, a
+// workgroup keeps a pair to itself and nothing is stored (Split, below).  Codes are read
+// past the caches where there are more than these hold (71 -> 65 us; a step of 64 MB that
+// the caches hold 25 -> 29).  Of earlier forms of this kernel, a walk of persistent waves,
+// the next item's codes on their way while one is computed, was 7% slower than one wave an
+// item, and three waves to a SIMD, for whose registers the next tile's codes come later, 1%.
 #include <type_traits>
 
 #include "uattn_internal.h"
@@ -170,8 +174,8 @@ constexpr int kCoherent = 16;  // the sc1 bit: stores to the device-coherent lev
 
 // Two blocks of heads at d = 128 take all registers of a SIMD; in 4 bits half of them
 // will do, with the queries in LDS and the next tile's codes in this tile's registers.
-// 17/1 heads of 10 x 1500-12000 keys 28.9 -> 25.6 us, 32/1 of 16 x 4000-8000
-// 30.2 -> 26.7; with 8 bits on either side registers spill (31.9 -> 34.0).
+// 10 x 1500-12000 keys, 136/8 heads 28.5 -> 25.5 us, 16 x 4000-8000, 128/4 30.2 -> 26.6;
+// with 8 bits on either side registers spill (keys 32.1 -> 34.2, values 32.4 -> 36.4).
 template <int D, int NB, int KB, int VB>
 constexpr bool kHalfSimd = NB == 2 && D == 128 && KB + VB == 8;
 
@@ -188,8 +192,9 @@ __global__ __launch_bounds__(64 * (kSplit == Split::kFused ? kTeamWaves : kSplit
   constexpr bool kFused = kSplit == Split::kFused, kTeam = kSplit == Split::kTeam, kChunks = !kFused && !kTeam;
   constexpr int kWaves = kFused ? kTeamWaves : kTeam ? kTurnWaves : 1;
   // The next tile's codes have registers of their own where there are enough.  kTeam, 256
-  // entries, 32/8 heads of 128: 4000 keys, keys in 4 bits, values in 8 320 us with, 307
-  // without; keys in 8, values in 4 271 and 281.  Of 64, 500-8000 keys, 8 bits: 226 and 237.
+  // entries, 32/8 heads of 128: 4000 keys, keys in 4 bits, values in 8 277 us with, 253
+  // without; 8 bits 354 and 331; keys in 8, values in 4 268 and 278.  Of 64, 500-8000 keys,
+  // 8 bits: 183 and 196.
   constexpr bool kQueriesInLds = kHalfSimd<D, NB, KB, VB>;
   constexpr bool kTwo = !kQueriesInLds && !(kTeam && D == 128 && VB == 8);
   // per wave: 32 keys' values on their way to the products; then (kFused) its partial
@@ -629,26 +634,33 @@ hipError_t launch(DecodeMxParams p, int num_cus, hipStream_t stream) {
       hipLaunchKernelGGL(kernel, dim3(n), dim3(64 * waves), 0, stream, p, p.seqlens, p.bt);
     });
   };
-  // Two blocks of heads at d = 128 have no registers (8 bits) or no room in LDS (4) for
-  // workgroups of more waves: chunks alone there.
+  // Two blocks of heads at d = 128 go by chunks alone.  Eight waves that fold in LDS have too
+  // few registers in 8 bits; in 4 they were no faster (16 entries of 300-2000 keys, 128/4
+  // heads 18.0 us by chunks, 19.0 folded).  A workgroup to a pair is not built there, though
+  // it fits (337 registers in 8 bits, 15 of them spilled in 4) and gains with many pairs: 256
+  // x 4000 keys, 136/8 heads 351 -> 286 us in 4 bits, 555 -> 491 in 8.
   if constexpr (NB == 1 || D == 64) {
     // Up to kTeamWaves chunks: one launch, nothing through memory.  A step of 700 keys,
-    // 32/8 heads, 8 bits 10.7 us with a merge, 9.1 so; 64 entries of 300-2000 keys, 32/8
-    // heads 58 and 44.
+    // 32/8 heads, 8 bits 11.0 us with a merge, 9.3 so; 64 entries of 300-2000 keys 44.3 and
+    // 41.6.
     if (p.nchunk_max > 1 && decode_mx_in_lds(p.nchunk_max, p.group, D))
       return run(decode_mx_kernel<D, NB, KB, VB, Split::kFused, 0>, pairs, p.nchunk_max);
-    // Many pairs: a workgroup to a pair.  256 entries of 4000 keys, 32/8 heads, 8 bits 436
-    // us with partials and their merge, 334 so; of 500-8000 keys in 4 bits 255, 244.  With
-    // 512 pairs the longest are too long for their workgroups (64 of 1280-16384: 199, 209).
+    // Many pairs: a workgroup to a pair.  256 entries of 4000 keys, 32/8 heads, 8 bits 430
+    // us with partials and their merge, 332 so; of 500-8000 keys in 4 bits 228, 217.  With
+    // 512 pairs the longest are too long for their workgroups (64 of 1280-16384, keys in 8
+    // bits, values in 4: 201, 209; of one length, which a launch does not know, 189, 150).
     if (p.nchunk_max > kTeamWaves && pairs >= 4 * static_cast<int64_t>(num_cus))
       return run(decode_mx_kernel<D, NB, KB, VB, Split::kTeam, kStreamed>, pairs, kTurnWaves);
   }
   // Codes go past the caches where the call may read more than half of what the last of
-  // them holds (256 MB): 8 x 32K keys 73 -> 68 us, 64 of 4000-8000, d = 64, 4 bits 56 -> 53; 10
-  // of 1500-12000, 136/8 heads (64 MB, bound 104) 28 -> 31.
+  // them holds (256 MB): 8 x 32K keys 71 -> 65 us, 64 of 4000-8000, d = 64, 4 bits 56 -> 53; 10
+  // of 1500-12000, 136/8 heads (64 MB, bound 104) 25 -> 29.
   const int64_t bytes = pairs * p.max_seqlen * (MxRow<D, KB>::kBytes + MxRow<D, VB>::kBytes + 2 * MxRow<D, KB>::kScales);
   // A wave to each chunk up to 32768 waves, as those without keys cost too: 64 entries of
-  // 500-1000 keys, 32/8 heads, 4 bits under a bound of 128K keys 68 us so, 26 with a walk.
+  // 500-1000 keys, 32/8 heads, 4 bits under a bound of 128K keys 68 us so, 26 with a walk
+  // (with one of 4096 waves 20, but 64 of 1280-16384 keys then 229, not 195).  The walk's
+  // bound says nothing of the lengths; it reads past the caches: 64 of 2000-4000 keys (209
+  // MB) 55 us, 59 through them; 64 of 500-1000 in 8 bits (101 MB, which they hold) 36 and 31.
   const int64_t most = pairs < kMostWaves ? kMostWaves / pairs : 1;
   p.stride = p.nchunk_max < most ? p.nchunk_max : static_cast<int>(most);
   const hipError_t e = p.stride < p.nchunk_max ? run(decode_mx_kernel<D, NB, KB, VB, Split::kWalk, kStreamed>, pairs * p.stride, 1)

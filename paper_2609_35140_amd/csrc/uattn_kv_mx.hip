@@ -71,7 +71,7 @@ __device__ __forceinline__ uint32_t block_scale(const u32x4& x) {
 
 // Write: a lane takes eight elements, four lanes a block, a wave the rows of one kv head of
 // 64 / (D / 8) consecutive tokens in each of its rounds.  24,000 tokens of 8 heads of 128: 26
-// us in 4 bits (123 MB, 4.7 TB/s), 30 in 8 (147 MB).  A lane to a block, without exchanges
+// us in 4 bits (123 MB, 4.7 TB/s), 29 in 8 (147 MB).  A lane to a block, without exchanges
 // and with scale bytes side by side: 26 and 32, as its loads, 64 bytes apart, cannot be
 // streamed; 64 tokens 2.8 us, so 2.6.
 constexpr int write_rounds(bool streamed) { return streamed ? 2 : 1; }
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void kv_write_mx_kernel(KvMxParams p) {
 
 // Read: a lane makes eight elements, a wave 64 / (D / 8) tokens' rows of one kv head
 // in each of its kRounds rounds.  A token without a place gets zeros.  64,000 tokens of 8
-// heads of 128, keys in 8 bits, values in 4 (365 MB): 70 us, 5.2 TB/s; 77 where the rows go
+// heads of 128, keys in 8 bits, values in 4 (365 MB): 68 us, 5.4 TB/s; 77 where the rows go
 // through the caches.
 constexpr int kRounds = 2;
 template <int D, int KB, int VB, bool kStreamed>
@@ -168,8 +168,8 @@ __device__ __forceinline__ bf16x8 round8(const u32x4& x) {
 
 // A workgroup takes `tokens` tokens of `pieces` 16-byte pieces each, kAhead pieces of a
 // lane on their way.  pieces is a multiple of 8, so a block's four lanes are of one row
-// and in or out of the range together.  39,855 tokens of 8 heads of 128 (326 MB): 56 us,
-// 5.8 TB/s; 62 through the caches.
+// and in or out of the range together.  39,855 tokens of 8 heads of 128 (326 MB): 55 us,
+// 5.9 TB/s; 62 through the caches.
 constexpr int round_ahead(bool streamed) { return streamed ? 2 : 1; }
 template <int KB, int VB, bool kStreamed>
 __global__ __launch_bounds__(256) void kv_round_mx_kernel(KvMxParams p, Divider pieces, int tokens) {
