@@ -1132,8 +1132,8 @@ def decode_mx(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, max
     out and lse as for :func:`decode`.  ``workspace``: decode_mx_workspace_bytes(...) bytes,
     whatever they hold; one is allocated when not given.  A decode's own may serve: which of its
     counters this call leaves zero is recorded, and :func:`decode` clears the others.  A graph's
-    replays record nothing: one that they share holds these bytes and the decode's counters
-    (counter_bytes) side by side.
+    replays and the runs of DecodeSteps neither record nor clear: one that they share holds
+    these bytes and the decode's counters (counter_bytes) side by side.
     """
     import torch
     dev = _gpu_of(q, "q")
